@@ -17,6 +17,9 @@
  * and, where the chunks are exchangeable, ifkv_chunk_counts + ifkv_reorder_chunks
  * derive a better chunk order from a first-stage selection.
  *
+ * What decoding needs after the path stands at the end: ifkv_rope_rows_axes (rotary positions with
+ * several axes), ifkv_store_pages, ifkv_attend_pages and ifkv_copy_pages (a paged cache in 8 bits).
+ *
  * General conventions
  * -------------------
  * - Every tensor is dense, row-major, [tokens, heads, head_dim], in the dtype of
@@ -357,6 +360,128 @@ int ifkv_chunk_counts(ifkv_ctx *ctx, const int32_t *idx, int64_t k, int32_t n_sl
  */
 int ifkv_reorder_chunks(ifkv_ctx *ctx, int32_t n_chunks, const int32_t *order_in, const int32_t *slot_counts,
                         const int32_t *chunk_len, int32_t *order_out);
+
+/*
+ * ifkv_rope_rows for positions with several axes (time, height and width of images and video):
+ * pair j of row r is turned by pos[r][axis_of_pair[j]] * theta_j.  Equal coordinates on all axes
+ * give what ifkv_rope_rows gives.  Angles are formed in fp64, the rotation runs in fp32 and is
+ * rounded once to the storage dtype.  In place.
+ *
+ *   x            device, row r at x + r * row_stride elements, its heads [n_heads, d] packed from
+ *                there on (the query and key heads of a fused projection's rows, for instance);
+ *                16-byte aligned, updated in place
+ *   pos          device int32 [n_rows, n_axes], any values
+ *   n_axes       1 .. IFKV_MAX_AXES
+ *   axis_of_pair host int32 [d/2], each in [0, n_axes); read before the call returns
+ *   row_stride   elements between rows, at least n_heads * d, a multiple of 16 bytes' worth; 0 = packed
+ * Errors: IFKV_EINVAL for NULL pointers, negative sizes, an axis out of range, misaligned x,
+ * a stride that does not fit.
+ */
+#define IFKV_MAX_AXES 8
+int ifkv_rope_rows_axes(ifkv_ctx *ctx, void *x, const int32_t *pos, int32_t n_axes, const int32_t *axis_of_pair,
+                        int64_t n_rows, int32_t n_heads, int64_t row_stride);
+
+/*
+ * Decoding from pages held in 8 bits
+ * ----------------------------------
+ * After the path the caches are read by decoding, token after token, for many sequences at once.
+ * The calls below keep them in pages of IFKV_PAGE_TOKENS tokens, in 8 bits an element: e4m3 (OCP, one
+ * sign, four exponent and three mantissa bits, largest 448, no infinity) times one scale for
+ * each page and kv head.  Scales are powers of two, so dividing by one is exact and every stored
+ * byte is the element rounded once, to the nearest e4m3 number at its scale (ties to even).
+ *
+ * Pages are shared by all sequences of a context's layer; page_table says which of them a sequence
+ * owns: token j of sequence s lies in page page_table[s * table_width + j / 64], slot j % 64.
+ * Entries outside [0, n_pages) name no page: rows written there are dropped, tokens there are not seen.
+ * A page that becomes free needs no call: kv_len of ifkv_store_pages says which of its tokens are kept.
+ *
+ *   k        device, byte [n_pages, H_kv, 64, d]
+ *   v        device, byte [n_pages, H_kv, d, 64]; token t of a page is byte
+ *              ((t >> 2) & 3) << 4 | (t >> 5) << 3 | ((t >> 4) & 1) << 2 | (t & 3)
+ *            of its 64: the 16 tokens whose products one lane of a matrix instruction takes are
+ *            16 bytes in a row
+ *   k_scale, v_scale  device float [n_pages, H_kv], powers of two
+ * All 16-byte aligned (scales 4).
+ */
+#define IFKV_PAGE_TOKENS 64
+typedef struct {
+  void *k;
+  void *v;
+  float *k_scale;
+  float *v_scale;
+  int64_t n_pages; /* fewer than 2^31 */
+} ifkv_page_cache;
+
+/*
+ * Writes key and value rows into the pages of their sequences: a finished context, the recomputed
+ * rows of one, the next token of every sequence of a batch.
+ *
+ * The rows of sequence s are row_start[s] .. row_start[s+1]-1; row r is token row_pos[r].  For
+ * every page that rows go to, and every kv head, with e = the smallest whole number >= -100 for
+ * which no finite element of those rows exceeds 448 * 2^e in magnitude:
+ *   - tokens below kv_len[s] that none of the rows replaces are kept.  If the page has any, its scale
+ *     becomes the larger of the old one and 2^e, and where that is larger than the old one the page's
+ *     bytes are rounded to it again;
+ *   - if it has none the scale becomes 2^e, and slots that no row fills become zero.
+ * An element that is not finite becomes NaN.  kv_len is not changed.
+ *
+ *   page_table  device int32 [n_seqs, table_width]
+ *   kv_len      device int32 [n_seqs]: tokens that sequence s holds before the call
+ *   row_start   device int32 [n_seqs + 1], ascending; rows behind row_start[n_seqs] are not used.
+ *               NULL: row r belongs to sequence r, n_rows == n_seqs
+ *   row_pos     device int32 [n_rows], ascending without repeats within a sequence; rows outside
+ *               [0, 64 * table_width) are dropped (and may stand at a sequence's end or beginning)
+ *   k_new, v_new  device, row r at k_new + r * k_stride elements, [H_kv, d] packed from there
+ *   k_stride, v_stride  elements between rows, at least H_kv * d, multiples of 16 bytes' worth; 0 = packed
+ * No two rows of a call may go to one slot, and no page of rows may be owned by two sequences.
+ * Errors: IFKV_EINVAL for NULL pointers, negative sizes, misalignment, strides that do not fit,
+ * n_rows != n_seqs without row_start; IFKV_ESHAPE if 64 * (table_width - 1) >= max_ctx or sizes reach 2^31.
+ */
+int ifkv_store_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t *page_table, int32_t n_seqs,
+                     int32_t table_width, const int32_t *kv_len, const int32_t *row_start, const int32_t *row_pos,
+                     int64_t n_rows, const void *k_new, const void *v_new, int64_t k_stride, int64_t v_stride);
+
+/*
+ * Causal attention of rows over the pages of their sequences: one row of each sequence when
+ * decoding, a few when proposed tokens are checked, many when a prompt arrives in pieces or rows of
+ * a finished context are recomputed.  For row r of sequence s with p = row_pos[r] and query head h:
+ *   out[r,h,:] = sum_{j <= p} softmax_j(sm_scale * q[r,h] . k[j,h/G]) * v[j,h/G,:]
+ * over the tokens that the pages hold.  The rows' own tokens have to be stored before.  What pages
+ * hold behind p, NaN included, does not show.  A row that sees a logit which is NaN or +infinity
+ * comes out as NaN.
+ *
+ * Logits, exponentials and sums are fp32; keys and values are exact in the products.  bf16 layers:
+ * queries enter the first product as they are, probabilities the second as the sum of two bf16
+ * numbers (16 bits; one, 8 bits, where sequences bring more than 64 query columns per kv head).  fp32
+ * layers: both as the sum of three.
+ *
+ *   row_start  as above; rows behind row_start[n_seqs] are neither read nor written in out and lse_out
+ *   max_rows   no sequence has more rows than this (1 without row_start); rows beyond are not computed
+ *   q          device, row r at q + r * q_stride elements, [H_q, d] packed from there, rotary embedding applied
+ *   q_stride   elements between rows, at least H_q * d, a multiple of 16 bytes' worth; 0 = packed
+ *   row_pos    device int32 [n_rows], in any order; rows outside [0, 64 * table_width), and rows that see
+ *              no token because the table names no page, produce zeros and an lse of -infinity
+ *   out        device [n_rows, H_q, d], packed; must not overlap q
+ *   lse_out    device float [n_rows, H_q]: natural-log sum-exp of the scaled logits of each row; may be NULL
+ *
+ * The first call allocates the context's memory for partial results of work cut along the cache
+ * (later ones allocate nothing); a caller that captures calls into a graph makes one call before.
+ * Errors: as ifkv_store_pages; IFKV_EINVAL for max_rows < 1; IFKV_ENOMEM.
+ */
+int ifkv_attend_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t *page_table, int32_t n_seqs,
+                      int32_t table_width, const int32_t *row_start, int32_t max_rows, const void *q, int64_t q_stride,
+                      const int32_t *row_pos, int64_t n_rows, void *out, float *lse_out);
+
+/*
+ * Copies pages onto other pages (keys, values and scales): page dst[i] becomes page src[i].  Forking a
+ * sequence shares its full pages in the table and copies the last one; compacting a pool moves its
+ * high pages into low free ones.
+ *
+ *   src, dst  host int32 [n], read before the call returns.  A page may be the source of many; no page may
+ *             be named twice in dst, or in both
+ * Errors: IFKV_EINVAL for NULL pointers, negative n, a page outside [0, n_pages), a page named twice; IFKV_ENOMEM.
+ */
+int ifkv_copy_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, int64_t n, const int32_t *src, const int32_t *dst);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,7 @@ import math
 import os
 import sys
 import warnings
-from typing import List, Optional, Sequence, Tuple
+from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -33,11 +33,13 @@ IFKV_F32, IFKV_BF16 = 0, 1
 IFKV_ROPE_HALF, IFKV_ROPE_INTERLEAVED = 0, 1
 IFKV_FLAG_FORCE_GENERIC = 1
 IFKV_FLAG_VALIDATE = 2
+IFKV_PAGE_TOKENS = 64
 
 EXPORTS = (
     "ifkv_create", "ifkv_destroy", "ifkv_last_error", "ifkv_version",
     "ifkv_reposition_keys", "ifkv_score_tokens", "ifkv_reposition_score", "ifkv_select_topk", "ifkv_select_topk_noalloc",
     "ifkv_recompute_attention", "ifkv_splice_kv", "ifkv_rope_rows", "ifkv_chunk_counts", "ifkv_reorder_chunks",
+    "ifkv_rope_rows_axes", "ifkv_store_pages", "ifkv_attend_pages", "ifkv_copy_pages",
     "ifkv_copy_bytes", "ifkv_mfma_probe", "ifkv_mfma_probe_sink_floats",   # include/ifkv_calibrate.h
     "ifkv_set_tuning", "ifkv_attention_plan",                                # include/ifkv_debug.h
 )
@@ -51,6 +53,23 @@ class LayerDesc(C.Structure):
         ("max_prompt", C.c_int32), ("flags", C.c_uint32),
         ("token_stride", C.c_int64), ("head_stride", C.c_int64),
     ]
+
+
+class PageCacheDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int64)]
+
+
+class PageCache(NamedTuple):
+    """Pages of 64 tokens in 8 bits (ifkv_page_cache): e4m3 numbers and a power-of-two scale for each page and kv head.
+    k [n_pages, H_kv, 64, d], v [n_pages, H_kv, d, 64] (float8_e4m3fn), k_scale and v_scale [n_pages, H_kv] (float32).
+    Token t of a page is byte VALUE_BYTE[t] of a value row."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+VALUE_BYTE = tuple(((t >> 2) & 3) << 4 | (t >> 5) << 3 | ((t >> 4) & 1) << 2 | (t & 3) for t in range(IFKV_PAGE_TOKENS))
 
 
 class IfkvError(RuntimeError):
@@ -106,6 +125,15 @@ def load_library() -> C.CDLL:
     lib.ifkv_chunk_counts.restype = C.c_int
     lib.ifkv_reorder_chunks.argtypes = [vp, i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
     lib.ifkv_reorder_chunks.restype = C.c_int
+    pc = C.POINTER(PageCacheDesc)
+    lib.ifkv_rope_rows_axes.argtypes = [vp, vp, vp, i32, vp, i64, i32, i64]
+    lib.ifkv_rope_rows_axes.restype = C.c_int
+    lib.ifkv_store_pages.argtypes = [vp, pc, vp, i32, i32, vp, vp, vp, i64, vp, vp, i64, i64]
+    lib.ifkv_store_pages.restype = C.c_int
+    lib.ifkv_attend_pages.argtypes = [vp, pc, vp, i32, i32, vp, i32, vp, i64, vp, i64, vp, vp]
+    lib.ifkv_attend_pages.restype = C.c_int
+    lib.ifkv_copy_pages.argtypes = [vp, pc, i64, vp, vp]
+    lib.ifkv_copy_pages.restype = C.c_int
     lib.ifkv_copy_bytes.argtypes = [vp, vp, vp, i64]
     lib.ifkv_copy_bytes.restype = C.c_int
     lib.ifkv_mfma_probe.argtypes = [vp, i32, i64, vp, C.POINTER(C.c_double)]
@@ -455,6 +483,106 @@ class Layer:
                                              self._packed(pos, "pos", (), dtype=torch.int32, rows=int(x.shape[0])),
                                              int(x.shape[0]), int(x.shape[1]))
         return x
+
+    # -- decoding from 8-bit pages ----------------------------------------------
+    def empty_pages(self, n_pages: int) -> PageCache:
+        """A pool of pages for this layer's shape; their contents are unspecified until store_pages or copy_pages writes them."""
+        n, h, d, f8 = int(n_pages), self.n_kv_heads, self.head_dim, torch.float8_e4m3fn
+        return PageCache(self._empty(n, h, IFKV_PAGE_TOKENS, d, dtype=f8), self._empty(n, h, d, IFKV_PAGE_TOKENS, dtype=f8),
+                         self._empty(n, h, dtype=torch.float32), self._empty(n, h, dtype=torch.float32))
+
+    def _pages(self, pages: PageCache) -> PageCacheDesc:
+        n, h, d, f8 = int(pages.k.shape[0]), self.n_kv_heads, self.head_dim, torch.float8_e4m3fn
+        desc = PageCacheDesc()
+        for name, t, tail, dtype in (("k", pages.k, (h, IFKV_PAGE_TOKENS, d), f8), ("v", pages.v, (h, d, IFKV_PAGE_TOKENS), f8),
+                                     ("k_scale", pages.k_scale, (h,), torch.float32), ("v_scale", pages.v_scale, (h,), torch.float32)):
+            if t.shape[0] != n:
+                raise ValueError(f"pages.{name}: {t.shape[0]} pages, pages.k has {n}")
+            setattr(desc, name, self._packed(t, "pages." + name, tail, dtype=dtype))
+        desc.n_pages = n
+        return desc
+
+    def _rows(self, t: torch.Tensor, name: str, heads: Optional[int], rows: Optional[int] = None) -> Tuple[int, int]:
+        """Address and row stride of rows [R, heads, d] whose heads lie packed; the rows may be slices of wider ones."""
+        if not t.is_cuda or t.dtype != self.torch_dtype:
+            raise ValueError(f"{name}: expected a {self.torch_dtype} tensor on the GPU, got {t.dtype} on {t.device}")
+        want = f"[{'R' if rows is None else rows}, {'n_heads' if heads is None else heads}, {self.head_dim}]"
+        if t.dim() != 3 or t.shape[2] != self.head_dim or (heads is not None and t.shape[1] != heads) or (rows is not None and t.shape[0] != rows):
+            raise ValueError(f"{name}: expected shape {want}, got {tuple(t.shape)}")
+        packed = t.shape[1] * self.head_dim
+        if t.shape[0] == 0:
+            return t.data_ptr(), packed
+        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim) or (t.shape[0] > 1 and t.stride(0) < packed):
+            raise ValueError(f"{name}: strides {tuple(t.stride())}: the heads of a row must be packed and rows must not overlap")
+        return t.data_ptr(), int(t.stride(0)) if t.shape[0] > 1 else packed
+
+    def _table(self, table: torch.Tensor, row_start: Optional[torch.Tensor], row_pos: torch.Tensor, n_rows: int):
+        if not table.is_cuda or table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError(f"table: expected a contiguous int32 tensor [S, W] on the GPU, got {table.dtype} {tuple(table.shape)} on {table.device}")
+        n_seqs = int(table.shape[0])
+        return (self._packed(table, "table", (int(table.shape[1]),), dtype=torch.int32), n_seqs, int(table.shape[1]),
+                self._packed(row_start, "row_start", (), dtype=torch.int32, rows=n_seqs + 1),
+                self._packed(row_pos, "row_pos", (), dtype=torch.int32, rows=n_rows))
+
+    def rope_rows_axes(self, x: torch.Tensor, pos: torch.Tensor, axes: torch.Tensor) -> torch.Tensor:
+        """In place; x [R, n_heads, d] (rows may be slices of wider ones), pos int32 [R, n_axes],
+        axes int32 [d/2] on the CPU: the axis that turns each pair."""
+        if axes.device.type != "cpu" or axes.dtype != torch.int32 or tuple(axes.shape) != (self.head_dim // 2,) or not axes.is_contiguous():
+            raise ValueError(f"axes: expected a contiguous int32 tensor [{self.head_dim // 2}] on the CPU, got {axes.dtype} {tuple(axes.shape)} on {axes.device}")
+        if pos.dim() != 2:
+            raise ValueError(f"pos: expected [R, n_axes], got {tuple(pos.shape)}")
+        n_rows, n_axes = int(x.shape[0]), int(pos.shape[1])
+        xp, stride = self._rows(x, "x", None)
+        self._invoke(self._lib.ifkv_rope_rows_axes, self._ctx, xp, self._packed(pos, "pos", (n_axes,), dtype=torch.int32, rows=n_rows),
+                     n_axes, axes.data_ptr(), n_rows, int(x.shape[1]), stride)
+        return x
+
+    def store_pages(self, pages: PageCache, table: torch.Tensor, kv_len: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                    row_pos: torch.Tensor, row_start: Optional[torch.Tensor] = None) -> None:
+        """Rows k_new, v_new [R, H_kv, d] -> the pages that table int32 [S, W] gives their sequences.  kv_len int32 [S]: tokens held
+        before.  row_start int32 [S + 1]: the rows of sequence s are row_start[s]..row_start[s+1]-1; None: one row a sequence."""
+        n = int(k_new.shape[0])
+        tp, n_seqs, width, sp, pp = self._table(table, row_start, row_pos, n)
+        (kp, ks), (vp, vs) = self._rows(k_new, "k_new", self.n_kv_heads), self._rows(v_new, "v_new", self.n_kv_heads, rows=n)
+        desc = self._pages(pages)
+        self._invoke(self._lib.ifkv_store_pages, self._ctx, C.byref(desc), tp, n_seqs, width,
+                     self._packed(kv_len, "kv_len", (), dtype=torch.int32, rows=n_seqs), sp, pp, n, kp, vp, ks, vs)
+
+    def attend_pages(self, q: torch.Tensor, row_pos: torch.Tensor, pages: PageCache, table: torch.Tensor,
+                     row_start: Optional[torch.Tensor] = None, max_rows: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                     return_lse: bool = False):
+        """Causal attention of q [R, H_q, d] at tokens row_pos int32 [R] over their sequences' pages.  max_rows: no sequence has more
+        rows than this (default: without row_start 1, with it all of them).  Rows behind row_start[S] of `out` stay as they were."""
+        n = int(q.shape[0])
+        if out is None:
+            out = self._empty(n, self.n_q_heads, self.head_dim)
+        lse = self._empty(n, self.n_q_heads, dtype=torch.float32) if return_lse else None
+        tp, n_seqs, width, sp, pp = self._table(table, row_start, row_pos, n)
+        qp, stride = self._rows(q, "q", self.n_q_heads)
+        desc = self._pages(pages)
+        if max_rows is None:
+            max_rows = 1 if row_start is None else max(n, 1)
+        self._invoke(self._lib.ifkv_attend_pages, self._ctx, C.byref(desc), tp, n_seqs, width, sp, int(max_rows), qp, stride, pp, n,
+                     self._packed(out, "out", (self.n_q_heads, self.head_dim), rows=n),
+                     self._packed(lse, "lse", (self.n_q_heads,), dtype=torch.float32, rows=n))
+        return (out, lse) if return_lse else out
+
+    def copy_pages(self, pages: PageCache, src: Union[torch.Tensor, Sequence[int]], dst: Union[torch.Tensor, Sequence[int]]) -> None:
+        """Page dst[i] becomes page src[i]; the lists are the host's (a sequence, or an int32 tensor on the CPU)."""
+        lists = []
+        for name, t in (("src", src), ("dst", dst)):
+            if not isinstance(t, torch.Tensor):
+                t = _i32_array(t)
+                lists.append((len(t), t))
+                continue
+            if t.device.type != "cpu" or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+                raise ValueError(f"{name}: expected a contiguous int32 tensor [n] on the CPU, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            lists.append((int(t.shape[0]), t.data_ptr()))
+        (n, src_p), (n_dst, dst_p) = lists
+        if n != n_dst:
+            raise ValueError(f"dst: {n_dst} entries, src has {n}")
+        desc = self._pages(pages)
+        self._invoke(self._lib.ifkv_copy_pages, self._ctx, C.byref(desc), n, src_p, dst_p)
 
     def chunk_counts(self, idx: torch.Tensor, slot_start: Sequence[int], n_ctx: int,
                      counts_out: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -73,6 +73,19 @@ int ensure_scratch(ifkv_ctx *ctx) {
   return IFKV_OK;
 }
 
+int ensure_page_partials(ifkv_ctx *ctx) {
+  const size_t bytes = ifkv::attend_pages_scratch_bytes(ctx);
+  if (ctx->page_partials != nullptr || bytes == 0) return IFKV_OK;
+  void *p = nullptr;
+  hipError_t e = hipMalloc(&p, bytes);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(ctx, IFKV_ENOMEM, "attend_pages: allocation of %zu bytes for partial results failed: %s", bytes, hipGetErrorString(e));
+  }
+  ctx->page_partials = p;
+  return IFKV_OK;
+}
+
 int ensure_inv_freq(ifkv_ctx *ctx) {
   if (ctx->d_inv_freq != nullptr) return IFKV_OK;
   const size_t bytes = sizeof(double) * (ctx->desc.head_dim / 2);
@@ -168,6 +181,7 @@ void ifkv_destroy(ifkv_ctx *ctx) {
   if (ctx->scratch != nullptr) (void)hipFree(ctx->scratch);
   if (ctx->score_arrived != nullptr) (void)hipFree(ctx->score_arrived);
   if (ctx->d_inv_freq != nullptr) (void)hipFree(ctx->d_inv_freq);
+  if (ctx->page_partials != nullptr) (void)hipFree(ctx->page_partials);
   delete ctx;
 }
 
@@ -528,6 +542,161 @@ int ifkv_reorder_chunks(ifkv_ctx *ctx, int32_t n_chunks, const int32_t *order_in
     return ca * (lb > 0 ? lb : 1) < cb * (la > 0 ? la : 1);
   });
   for (int32_t s = 0; s < n_chunks; ++s) order_out[s] = order[slot[s]];
+  return IFKV_OK;
+}
+
+namespace {
+
+// Elements between rows of a tensor whose rows hold `row` packed elements; 0 asks for the packed layout.
+bool row_stride_ok(const ifkv_ctx *ctx, int64_t row, int64_t *stride) {
+  if (*stride == 0) *stride = row;
+  return *stride >= row && *stride % static_cast<int64_t>(16 / ifkv::dtype_size(ctx->desc.dtype)) == 0 && *stride <= (int64_t(1) << 40);
+}
+
+int pages_validate(ifkv_ctx *ctx, const char *what, const ifkv_page_cache *pages) {
+  if (pages == nullptr) return fail(ctx, IFKV_EINVAL, "%s: pages is NULL", what);
+  if (pages->n_pages < 0) return fail(ctx, IFKV_EINVAL, "%s: n_pages is negative", what);
+  if (pages->n_pages >= (int64_t(1) << 31)) return fail(ctx, IFKV_ESHAPE, "%s: too many pages", what);
+  if (pages->n_pages > 0 && (pages->k == nullptr || pages->v == nullptr || pages->k_scale == nullptr || pages->v_scale == nullptr))
+    return fail(ctx, IFKV_EINVAL, "%s: NULL pointer in pages", what);
+  if (!aligned16(pages->k) || !aligned16(pages->v))
+    return fail(ctx, IFKV_EINVAL, "%s: pages must be 16-byte aligned", what);
+  return IFKV_OK;
+}
+
+// What the calls that go through a page table have in common.
+int page_table_validate(ifkv_ctx *ctx, const char *what, const ifkv_page_cache *pages, const ifkv::PageTable &t) {
+  int rc = pages_validate(ctx, what, pages);
+  if (rc != IFKV_OK) return rc;
+  if (t.n_seqs < 0 || t.width < 0 || t.n_rows < 0) return fail(ctx, IFKV_EINVAL, "%s: negative size", what);
+  if (t.n_rows >= (int64_t(1) << 31)) return fail(ctx, IFKV_ESHAPE, "%s: too many rows", what);
+  if ((static_cast<int64_t>(t.width) - 1) * IFKV_PAGE_TOKENS >= ctx->desc.max_ctx)
+    return fail(ctx, IFKV_ESHAPE, "%s: %d pages of a sequence exceed max_ctx=%lld", what, t.width,
+                static_cast<long long>(ctx->desc.max_ctx));
+  if (t.row_start == nullptr && t.n_rows != t.n_seqs)
+    return fail(ctx, IFKV_EINVAL, "%s: without row_start every sequence has one row, got %lld rows of %d sequences", what,
+                static_cast<long long>(t.n_rows), t.n_seqs);
+  if (t.n_rows > 0 && t.n_seqs > 0 && (t.row_pos == nullptr || (t.width > 0 && t.table == nullptr)))
+    return fail(ctx, IFKV_EINVAL, "%s: NULL pointer", what);
+  return IFKV_OK;
+}
+
+}  // namespace
+
+int ifkv_rope_rows_axes(ifkv_ctx *ctx, void *x, const int32_t *pos, int32_t n_axes, const int32_t *axis_of_pair, int64_t n_rows,
+                        int32_t n_heads, int64_t row_stride) {
+  if (ctx == nullptr) return IFKV_EINVAL;
+  if (n_rows < 0 || n_heads <= 0) return fail(ctx, IFKV_EINVAL, "rope_rows_axes: n_rows must be >= 0 and n_heads > 0");
+  if (n_rows >= (int64_t(1) << 31)) return fail(ctx, IFKV_ESHAPE, "rope_rows_axes: too many rows");
+  if (n_axes < 1 || n_axes > IFKV_MAX_AXES)
+    return fail(ctx, IFKV_EINVAL, "rope_rows_axes: n_axes=%d is outside [1, %d]", n_axes, IFKV_MAX_AXES);
+  if (axis_of_pair == nullptr) return fail(ctx, IFKV_EINVAL, "rope_rows_axes: axis_of_pair is NULL");
+  ifkv::PairAxes axes = {};
+  for (int j = 0; j < ctx->desc.head_dim / 2; ++j) {
+    if (axis_of_pair[j] < 0 || axis_of_pair[j] >= n_axes)
+      return fail(ctx, IFKV_EINVAL, "rope_rows_axes: axis_of_pair[%d]=%d is outside [0, %d)", j, axis_of_pair[j], n_axes);
+    axes.axis[j] = static_cast<uint8_t>(axis_of_pair[j]);
+  }
+  if (!row_stride_ok(ctx, static_cast<int64_t>(n_heads) * ctx->desc.head_dim, &row_stride))
+    return fail(ctx, IFKV_EINVAL, "rope_rows_axes: row_stride=%lld does not fit rows of %d heads", static_cast<long long>(row_stride),
+                n_heads);
+  if (n_rows == 0) return IFKV_OK;
+  if (x == nullptr || pos == nullptr) return fail(ctx, IFKV_EINVAL, "rope_rows_axes: NULL pointer");
+  if (!aligned16(x)) return fail(ctx, IFKV_EINVAL, "rope_rows_axes: x must be 16-byte aligned");
+  int rc = ensure_inv_freq(ctx);
+  if (rc != IFKV_OK) return rc;
+  hipError_t e = ifkv::launch_rope_rows_axes(ctx, x, pos, n_axes, axes, n_rows, n_heads, row_stride);
+  return e == hipSuccess ? IFKV_OK : hip_fail(ctx, e, "rope_rows_axes kernel launch");
+}
+
+int ifkv_store_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t *page_table, int32_t n_seqs, int32_t table_width,
+                     const int32_t *kv_len, const int32_t *row_start, const int32_t *row_pos, int64_t n_rows, const void *k_new,
+                     const void *v_new, int64_t k_stride, int64_t v_stride) {
+  if (ctx == nullptr) return IFKV_EINVAL;
+  const ifkv::PageTable t = {page_table, row_start, row_pos, n_rows, n_seqs, table_width};
+  int rc = page_table_validate(ctx, "store_pages", pages, t);
+  if (rc != IFKV_OK) return rc;
+  const int64_t row = static_cast<int64_t>(ctx->desc.n_kv_heads) * ctx->desc.head_dim;
+  if (!row_stride_ok(ctx, row, &k_stride) || !row_stride_ok(ctx, row, &v_stride))
+    return fail(ctx, IFKV_EINVAL, "store_pages: strides (%lld, %lld) do not fit rows of %lld elements", static_cast<long long>(k_stride),
+                static_cast<long long>(v_stride), static_cast<long long>(row));
+  if (n_rows == 0 || n_seqs == 0) return IFKV_OK;
+  if (kv_len == nullptr || k_new == nullptr || v_new == nullptr) return fail(ctx, IFKV_EINVAL, "store_pages: NULL pointer");
+  if (!aligned16(k_new) || !aligned16(v_new)) return fail(ctx, IFKV_EINVAL, "store_pages: rows must be 16-byte aligned");
+  if (table_width == 0 || pages->n_pages == 0) return IFKV_OK;  // no page: every row is dropped
+  if (ctx->desc.flags & IFKV_FLAG_VALIDATE) {
+    rc = ensure_scratch(ctx);
+    if (rc != IFKV_OK) return rc;
+    int64_t bad = -1;
+    hipError_t ev = ifkv::validate_page_rows(ctx, t, &bad);
+    if (ev != hipSuccess) return hip_fail(ctx, ev, "row_pos check");
+    if (bad >= 0)
+      return fail(ctx, IFKV_EINVAL, "store_pages: row_pos is not strictly ascending within its sequence at index %lld",
+                  static_cast<long long>(bad));
+  }
+  hipError_t e = ifkv::launch_store_pages(ctx, *pages, t, kv_len, k_new, v_new, k_stride, v_stride);
+  return e == hipSuccess ? IFKV_OK : hip_fail(ctx, e, "store_pages kernel launch");
+}
+
+int ifkv_attend_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t *page_table, int32_t n_seqs, int32_t table_width,
+                      const int32_t *row_start, int32_t max_rows, const void *q, int64_t q_stride, const int32_t *row_pos,
+                      int64_t n_rows, void *out, float *lse_out) {
+  if (ctx == nullptr) return IFKV_EINVAL;
+  const ifkv::PageTable t = {page_table, row_start, row_pos, n_rows, n_seqs, table_width};
+  int rc = page_table_validate(ctx, "attend_pages", pages, t);
+  if (rc != IFKV_OK) return rc;
+  if (max_rows < 1) return fail(ctx, IFKV_EINVAL, "attend_pages: max_rows=%d must be at least 1", max_rows);
+  if (row_start == nullptr) max_rows = 1;
+  if (max_rows > n_rows) max_rows = static_cast<int32_t>(n_rows);
+  const int64_t row = static_cast<int64_t>(ctx->desc.n_q_heads) * ctx->desc.head_dim;
+  if (!row_stride_ok(ctx, row, &q_stride))
+    return fail(ctx, IFKV_EINVAL, "attend_pages: q_stride=%lld does not fit rows of %lld elements", static_cast<long long>(q_stride),
+                static_cast<long long>(row));
+  if (n_rows == 0 || n_seqs == 0) return IFKV_OK;
+  if (q == nullptr || out == nullptr) return fail(ctx, IFKV_EINVAL, "attend_pages: NULL pointer");
+  if (!aligned16(q) || !aligned16(out)) return fail(ctx, IFKV_EINVAL, "attend_pages: tensors must be 16-byte aligned");
+  rc = ensure_page_partials(ctx);
+  if (rc != IFKV_OK) return rc;
+  hipError_t e = ifkv::launch_attend_pages(ctx, *pages, t, max_rows, q, q_stride, out, lse_out);
+  return e == hipSuccess ? IFKV_OK : hip_fail(ctx, e, "attend_pages kernel launch");
+}
+
+int ifkv_copy_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, int64_t n, const int32_t *src, const int32_t *dst) {
+  if (ctx == nullptr) return IFKV_EINVAL;
+  int rc = pages_validate(ctx, "copy_pages", pages);
+  if (rc != IFKV_OK) return rc;
+  if (n < 0) return fail(ctx, IFKV_EINVAL, "copy_pages: n is negative");
+  if (n == 0) return IFKV_OK;
+  if (src == nullptr || dst == nullptr) return fail(ctx, IFKV_EINVAL, "copy_pages: NULL pointer");
+  if (n > pages->n_pages)
+    return fail(ctx, IFKV_EINVAL, "copy_pages: %lld copies among %lld pages name one twice", static_cast<long long>(n),
+                static_cast<long long>(pages->n_pages));
+  for (int64_t i = 0; i < n; ++i)
+    if (src[i] < 0 || src[i] >= pages->n_pages || dst[i] < 0 || dst[i] >= pages->n_pages)
+      return fail(ctx, IFKV_EINVAL, "copy_pages: copy %lld (%d -> %d) is outside [0, %lld)", static_cast<long long>(i), src[i], dst[i],
+                  static_cast<long long>(pages->n_pages));
+  try {
+    std::vector<uint64_t> written((pages->n_pages + 63) / 64);  // one bit a page
+    for (int64_t i = 0; i < n; ++i) {
+      uint64_t &word = written[dst[i] >> 6];
+      const uint64_t bit = uint64_t(1) << (dst[i] & 63);
+      if (word & bit) return fail(ctx, IFKV_EINVAL, "copy_pages: page %d is named twice in dst", dst[i]);
+      word |= bit;
+    }
+    for (int64_t i = 0; i < n; ++i)
+      if (written[src[i] >> 6] >> (src[i] & 63) & 1)
+        return fail(ctx, IFKV_EINVAL, "copy_pages: page %d is named in src and in dst", src[i]);
+  } catch (const std::bad_alloc &) {
+    return fail(ctx, IFKV_ENOMEM, "copy_pages: out of host memory");
+  }
+  for (int64_t i = 0; i < n; i += ifkv::kPagePairs) {
+    const int m = static_cast<int>(std::min<int64_t>(n - i, ifkv::kPagePairs));
+    ifkv::PagePairs pairs;
+    std::copy_n(src + i, m, pairs.src);
+    std::copy_n(dst + i, m, pairs.dst);
+    hipError_t e = ifkv::launch_copy_pages(ctx, *pages, pairs, m);
+    if (e != hipSuccess) return hip_fail(ctx, e, "copy_pages kernel launch");
+  }
   return IFKV_OK;
 }
 

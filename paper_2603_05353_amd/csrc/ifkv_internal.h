@@ -30,6 +30,7 @@ struct ifkv_ctx {
   double *d_inv_freq = nullptr; // device copy, uploaded on first use
   void *scratch = nullptr;      // device scratch shared by the stages, allocated once
   size_t scratch_bytes = 0;
+  void *page_partials = nullptr; // paged attention: partial results of work that is cut along the cache, allocated once
   int *score_arrived = nullptr; // stage 2: blocks of a key range that have finished; zero between launches
   std::string err;
 };
@@ -115,5 +116,36 @@ hipError_t launch_mfma_probe(ifkv_ctx *ctx, int pattern, int iters, float *sink)
 
 // Rotary embedding of recomputed rows at given positions, in place.
 hipError_t launch_rope_rows(ifkv_ctx *ctx, void *x, const int32_t *pos, int64_t n_rows, int n_heads);
+
+// The same for positions with several axes; the axis of every pair travels in the kernel arguments.
+struct PairAxes {
+  uint8_t axis[kMaxHeadDim / 2];
+};
+hipError_t launch_rope_rows_axes(ifkv_ctx *ctx, void *x, const int32_t *pos, int n_axes, const PairAxes &axes, int64_t n_rows,
+                                 int n_heads, int64_t row_stride);
+
+// ---- pages of 64 tokens in 8 bits (pages.hip, attention_pages.hip) ----------
+struct PageTable {
+  const int32_t *table;      // [n_seqs, width]
+  const int32_t *row_start;  // [n_seqs + 1], or null: row r belongs to sequence r
+  const int32_t *row_pos;    // [n_rows]
+  int64_t n_rows;
+  int32_t n_seqs, width;
+};
+hipError_t launch_store_pages(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, const int32_t *kv_len,
+                              const void *k_new, const void *v_new, int64_t k_stride, int64_t v_stride);
+hipError_t launch_attend_pages(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int32_t max_rows, const void *q,
+                               int64_t q_stride, void *out, float *lse_out);
+size_t attend_pages_scratch_bytes(const ifkv_ctx *ctx);
+
+// debug mode: row_pos strictly ascending within every sequence
+hipError_t validate_page_rows(ifkv_ctx *ctx, const PageTable &t, int64_t *bad_out);
+
+// Pairs of pages travel by value too.
+constexpr int kPagePairs = 448;
+struct PagePairs {
+  int32_t src[kPagePairs], dst[kPagePairs];
+};
+hipError_t launch_copy_pages(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PagePairs &pairs, int n);
 
 }  // namespace ifkv

@@ -318,6 +318,91 @@ __global__ __launch_bounds__(kThreads) void rope_rows_kernel(v4u *__restrict__ x
   }
 }
 
+// ---------------------------------------------------------------------------
+// The same rotation for positions with several axes: the angle of pair j is pos[r][axis[j]] * theta_j.
+// A workgroup owns rows_per_block rows.  Its loads go out first; the (cos, sin) tables of its rows are formed, one angle a
+// thread, while they are on their way.
+// ---------------------------------------------------------------------------
+constexpr int kAxesAngles = kThreads;  // angles of a workgroup: rows_per_block * d/2 at most
+
+template <typename Tag, int PAIRING>
+__global__ __launch_bounds__(kThreads) void rope_rows_axes_kernel(char *__restrict__ x, const int32_t *__restrict__ pos,
+                                                                  const double *__restrict__ inv_freq, PairAxes axes, int n_axes,
+                                                                  int64_t n_rows, int rows_per_block, int n_heads, int half_shift,
+                                                                  int64_t row_bytes) {
+  using E = Elem<Tag>;
+  constexpr int VE = E::kVec;
+  constexpr bool HALF = PAIRING == IFKV_ROPE_HALF;
+  constexpr int LOADS = HALF ? 2 : 1;  // vectors of an item: both halves of VE pairs, or VE/2 adjacent pairs
+  __shared__ float s_cos[kAxesAngles];
+  __shared__ float s_sin[kAxesAngles];
+  const int tid = threadIdx.x;
+  const int half = 1 << half_shift;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows_per_block;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(rows_per_block), n_rows - row0));
+  const int per_head = HALF ? half / VE : 2 * half / VE;
+  const int per_row = n_heads * per_head;
+  const int items = rows * per_row;
+  char *base = x + row0 * row_bytes;
+
+  bool first = true;
+  for (int it0 = 0; it0 < items; it0 += kThreads * kBatch) {
+    v4u *at[kBatch];
+    v4u in[kBatch][LOADS];
+    int angle[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int it = it0 + u * kThreads + tid;
+      at[u] = nullptr;
+      if (it >= items) continue;
+      const int r = it / per_row, c = it - r * per_row;
+      const int h = c / per_head, v = c - h * per_head;
+      at[u] = reinterpret_cast<v4u *>(base + r * row_bytes) + h * (2 * half / VE) + v;
+      angle[u] = (r << half_shift) + v * (HALF ? VE : VE / 2);
+      in[u][0] = at[u][0];
+      if constexpr (HALF) in[u][1] = at[u][per_head];
+    }
+    if (first) {
+      for (int a = tid; a < rows << half_shift; a += kThreads) {
+        const int r = a >> half_shift, j = a & (half - 1);
+        double sn, cs;
+        sincos(static_cast<double>(pos[(row0 + r) * n_axes + axes.axis[j]]) * inv_freq[j], &sn, &cs);
+        s_cos[a] = static_cast<float>(cs);
+        s_sin[a] = static_cast<float>(sn);
+      }
+      __syncthreads();
+      first = false;
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (at[u] == nullptr) continue;
+      if constexpr (HALF) {
+        float a[VE], b[VE], ra[VE], rb[VE];
+        E::unpack(in[u][0], a);
+        E::unpack(in[u][1], b);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const float cs = s_cos[angle[u] + e], sn = s_sin[angle[u] + e];
+          ra[e] = fmaf(a[e], cs, -(b[e] * sn));
+          rb[e] = fmaf(a[e], sn, b[e] * cs);
+        }
+        at[u][0] = E::pack(ra);
+        at[u][per_head] = E::pack(rb);
+      } else {
+        float f[VE], r[VE];
+        E::unpack(in[u][0], f);
+#pragma unroll
+        for (int e = 0; e < VE / 2; ++e) {
+          const float cs = s_cos[angle[u] + e], sn = s_sin[angle[u] + e];
+          r[2 * e] = fmaf(f[2 * e], cs, -(f[2 * e + 1] * sn));
+          r[2 * e + 1] = fmaf(f[2 * e], sn, f[2 * e + 1] * cs);
+        }
+        at[u][0] = E::pack(r);
+      }
+    }
+  }
+}
+
 // Plain streaming copy with the same access shape (calibration only).
 __global__ __launch_bounds__(kThreads) void copy_kernel(v4u *__restrict__ dst, const v4u *__restrict__ src,
                                                         int64_t n_vecs) {
@@ -407,6 +492,43 @@ hipError_t launch_rope_rows(ifkv_ctx *ctx, void *x, const int32_t *pos, int64_t 
   }
 #undef IFKV_LAUNCH_ROPE
   return hipGetLastError();
+}
+
+hipError_t launch_rope_rows_axes(ifkv_ctx *ctx, void *x, const int32_t *pos, int n_axes, const PairAxes &axes, int64_t n_rows,
+                                 int n_heads, int64_t row_stride) {
+  if (n_rows <= 0 || n_heads <= 0) return hipSuccess;
+  const auto &d = ctx->desc;
+  const int half = d.head_dim / 2, half_shift = __builtin_ctz(half);
+  // a workgroup of as many rows as it has threads for angles, as soon as those fill the chip
+  const int most = kAxesAngles / half;
+  const int rows_per_block = n_rows >= 1024 * most ? most : 1;
+  const int64_t row_bytes = row_stride * static_cast<int64_t>(dtype_size(d.dtype));
+  // a grid has fewer than 2^32 threads
+  const int64_t rows_per_launch = int64_t(rows_per_block) << 23;
+  for (int64_t r0 = 0; r0 < n_rows; r0 += rows_per_launch) {
+    const int64_t nr = std::min(n_rows - r0, rows_per_launch);
+    dim3 grid(static_cast<unsigned>((nr + rows_per_block - 1) / rows_per_block)), block(kThreads);
+    char *xr = static_cast<char *>(x) + r0 * row_bytes;
+    const int32_t *pr = pos + r0 * n_axes;
+#define IFKV_LAUNCH_AXES(TAG, PAIR)                                                                                                  \
+  hipLaunchKernelGGL((rope_rows_axes_kernel<TAG, PAIR>), grid, block, 0, ctx->stream, xr, pr, ctx->d_inv_freq, axes, n_axes, nr,    \
+                     rows_per_block, n_heads, half_shift, row_bytes)
+    if (d.dtype == IFKV_BF16) {
+      if (d.pairing == IFKV_ROPE_HALF)
+        IFKV_LAUNCH_AXES(BF16Tag, IFKV_ROPE_HALF);
+      else
+        IFKV_LAUNCH_AXES(BF16Tag, IFKV_ROPE_INTERLEAVED);
+    } else {
+      if (d.pairing == IFKV_ROPE_HALF)
+        IFKV_LAUNCH_AXES(F32Tag, IFKV_ROPE_HALF);
+      else
+        IFKV_LAUNCH_AXES(F32Tag, IFKV_ROPE_INTERLEAVED);
+    }
+#undef IFKV_LAUNCH_AXES
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_copy(ifkv_ctx *ctx, void *dst, const void *src, int64_t n_bytes) {

@@ -23,6 +23,15 @@ __global__ void check_ascending_kernel(const int32_t *__restrict__ v, int64_t n,
     if (v[i] <= v[i - 1]) atomicMin(first_bad, static_cast<int>(i));
 }
 
+// first_bad: smallest i that is not above the entry before it in the same sequence; negative entries name no token
+__global__ void check_page_rows_kernel(PageTable t, int *first_bad) {
+  for (int64_t s = blockIdx.x; s < t.n_seqs; s += gridDim.x) {
+    const int64_t lo = max(t.row_start[s], 0), hi = min(static_cast<int64_t>(t.row_start[s + 1]), t.n_rows);
+    for (int64_t i = lo + 1 + threadIdx.x; i < hi; i += blockDim.x)
+      if (t.row_pos[i] >= 0 && t.row_pos[i] <= t.row_pos[i - 1]) atomicMin(first_bad, static_cast<int>(i));
+  }
+}
+
 // first_bad: smallest i whose row was also named by another entry (the later of the two in the
 // order the hardware happened to process them, so "a" duplicate, not "the first" one);
 // rows outside [0, n_kv) are skipped, as the splice skips them
@@ -67,6 +76,17 @@ hipError_t validate_ascending(ifkv_ctx *ctx, const int32_t *v, int64_t n, int64_
   hipLaunchKernelGGL(fill_words_kernel, dim3(1), dim3(64), 0, ctx->stream, reinterpret_cast<uint32_t *>(flag), int64_t(1),
                      static_cast<uint32_t>(INT_MAX));
   hipLaunchKernelGGL(check_ascending_kernel, dim3(blocks_for(n)), dim3(256), 0, ctx->stream, v, n, flag);
+  hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : read_flag(ctx, flag, bad_out);
+}
+
+hipError_t validate_page_rows(ifkv_ctx *ctx, const PageTable &t, int64_t *bad_out) {
+  *bad_out = -1;
+  if (t.row_start == nullptr || t.n_seqs < 1) return hipSuccess;
+  int *flag = static_cast<int *>(ctx->scratch);
+  hipLaunchKernelGGL(fill_words_kernel, dim3(1), dim3(64), 0, ctx->stream, reinterpret_cast<uint32_t *>(flag), int64_t(1),
+                     static_cast<uint32_t>(INT_MAX));
+  hipLaunchKernelGGL(check_page_rows_kernel, dim3(t.n_seqs < 2048 ? t.n_seqs : 2048), dim3(256), 0, ctx->stream, t, flag);
   hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : read_flag(ctx, flag, bad_out);
 }
