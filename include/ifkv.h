@@ -456,7 +456,8 @@ int ifkv_store_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t 
  * layers: both as the sum of three.
  *
  *   row_start  as above; rows behind row_start[n_seqs] are neither read nor written in out and lse_out
- *   max_rows   no sequence has more rows than this (1 without row_start); rows beyond are not computed
+ *   max_rows   no sequence has more rows than this (1 without row_start); rows beyond are not computed.  The work that a
+ *              call is divided into follows it: a bound near the true number is worth giving.  max_rows * G <= 2^27
  *   q          device, row r at q + r * q_stride elements, [H_q, d] packed from there, rotary embedding applied
  *   q_stride   elements between rows, at least H_q * d, a multiple of 16 bytes' worth; 0 = packed
  *   row_pos    device int32 [n_rows], in any order; rows outside [0, 64 * table_width), and rows that see

@@ -1,10 +1,10 @@
 // Causal attention of rows over 8-bit pages.
 //
-// This file holds the dispatcher and the plain fp32 ALU kernel (contexts created with IFKV_FLAG_FORCE_GENERIC, cross-checking).
+// This file holds the dispatcher and the plain fp32 ALU kernel (contexts created with IFKV_FLAG_FORCE_GENERIC, cross-checking).  The
+// matrix kernels live in attention_pages_matrix.hip.
 #include <algorithm>
 
-#include "ifkv_device.h"
-#include "pages.h"
+#include "attention_pages.h"
 
 namespace ifkv {
 
@@ -108,13 +108,8 @@ hipError_t run_generic(ifkv_ctx *ctx, const ifkv_page_cache &pages, PageTable t,
   const int step = std::max(1, (1 << 23) / max_rows);
   const int64_t e = static_cast<int64_t>(dtype_size(d.dtype));
   for (int s = 0; s < t.n_seqs; s += step) {
-    PageTable u = t;
-    u.n_seqs = std::min(step, t.n_seqs - s);
-    u.table += static_cast<int64_t>(s) * t.width;
-    if (t.row_start != nullptr) u.row_start += s;
-    const int64_t skip = t.row_start != nullptr ? 0 : s;  // one row of each sequence
-    u.row_pos += skip;
-    u.n_rows -= skip;
+    const PageTable u = t.from(s, std::min(step, t.n_seqs - s));
+    const int64_t skip = t.row_start != nullptr ? 0 : s;  // rows of the sequences before, where each has one
     hipLaunchKernelGGL((attend_pages_generic_kernel<Tag, D>), dim3(static_cast<unsigned>(u.n_seqs) * max_rows, d.n_q_heads), dim3(kThreads),
                        0, ctx->stream, u, max_rows, static_cast<const uint8_t *>(pages.k), static_cast<const uint8_t *>(pages.v),
                        pages.k_scale, pages.v_scale, static_cast<int>(pages.n_pages), d.n_q_heads, d.n_kv_heads, ctx->sm_scale,
@@ -126,11 +121,14 @@ hipError_t run_generic(ifkv_ctx *ctx, const ifkv_page_cache &pages, PageTable t,
 
 }  // namespace
 
-size_t attend_pages_scratch_bytes(const ifkv_ctx *) { return 0; }
+size_t attend_pages_scratch_bytes(const ifkv_ctx *ctx) {
+  return ctx->desc.flags & IFKV_FLAG_FORCE_GENERIC ? 0 : attend_matrix_scratch_bytes(ctx);
+}
 
 hipError_t launch_attend_pages(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int32_t max_rows, const void *q,
                                int64_t q_stride, void *out, float *lse_out) {
   const auto &d = ctx->desc;
+  if (!(d.flags & IFKV_FLAG_FORCE_GENERIC)) return launch_attend_matrix(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if (d.dtype == IFKV_BF16) {
     if (d.head_dim == 128) return run_generic<BF16Tag, 128>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
     return run_generic<BF16Tag, 64>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);

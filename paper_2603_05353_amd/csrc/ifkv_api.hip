@@ -648,6 +648,8 @@ int ifkv_attend_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t
   if (max_rows < 1) return fail(ctx, IFKV_EINVAL, "attend_pages: max_rows=%d must be at least 1", max_rows);
   if (row_start == nullptr) max_rows = 1;
   if (max_rows > n_rows) max_rows = static_cast<int32_t>(n_rows);
+  if (static_cast<int64_t>(max_rows) * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads) > (int64_t(1) << 27))
+    return fail(ctx, IFKV_ESHAPE, "attend_pages: %d rows of a sequence are too many", max_rows);
   const int64_t row = static_cast<int64_t>(ctx->desc.n_q_heads) * ctx->desc.head_dim;
   if (!row_stride_ok(ctx, row, &q_stride))
     return fail(ctx, IFKV_EINVAL, "attend_pages: q_stride=%lld does not fit rows of %lld elements", static_cast<long long>(q_stride),

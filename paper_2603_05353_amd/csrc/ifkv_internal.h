@@ -131,6 +131,12 @@ struct PageTable {
   const int32_t *row_pos;    // [n_rows]
   int64_t n_rows;
   int32_t n_seqs, width;
+  // `n` sequences from s on; without row_start their rows are the first of what follows
+  PageTable from(int s, int n) const {
+    const int64_t skip = row_start != nullptr ? 0 : s;
+    return PageTable{table + static_cast<int64_t>(s) * width, row_start != nullptr ? row_start + s : nullptr, row_pos + skip, n_rows - skip,
+                     n, width};
+  }
 };
 hipError_t launch_store_pages(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, const int32_t *kv_len,
                               const void *k_new, const void *v_new, int64_t k_stride, int64_t v_stride);
