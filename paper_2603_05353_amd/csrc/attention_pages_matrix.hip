@@ -42,16 +42,18 @@ struct Image {
   float ref[NT][16], sum[NT][16];
 };
 
-template <typename Tag, int D>
-__device__ __forceinline__ void write_columns(void *out, float *lse_out, int64_t row_head, int g, const f32x4 *o, int stride, float ref, float sum) {
+// DT blocks of 16 output rows of a column, from block dt0 on.
+template <typename Tag, int D, int DT>
+__device__ __forceinline__ void write_columns(void *out, float *lse_out, int64_t row_head, int dt0, int g, const f32x4 *o, int stride, float ref,
+                                              float sum) {
   // a column without any token: zeros, and the logarithm of nothing
   const float inv = 1.f / sum;
 #pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) {
+  for (int dt = 0; dt < DT; ++dt) {
     f32x4 x = o[dt * stride];
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = ref == -INFINITY ? 0.f : x[e] * inv;
-    const int64_t at = row_head * D + dt * 16 + g * 4;
+    const int64_t at = row_head * D + (dt0 + dt) * 16 + g * 4;
     if constexpr (Elem<Tag>::kBytes == 2) {
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
       *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(out) + at) =
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_pages_
   if (part.n_parts == 1) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
-      if (real[nt]) write_columns<Tag, D>(out, lse_out, row_head[nt], g, &o[0][nt], NT, pos[nt] == INT32_MAX ? -INFINITY : ref[nt], sum[nt]);
+      if (real[nt]) write_columns<Tag, D, DT>(out, lse_out, row_head[nt], 0, g, &o[0][nt], NT, pos[nt] == INT32_MAX ? -INFINITY : ref[nt], sum[nt]);
     return;
   }
   Image<D, NT> &im = partials[static_cast<int64_t>(h) * 2 * plan.target_parts + part.slot];
@@ -364,40 +366,99 @@ __global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_pages_
   }
 }
 
-// Joins the parts of an item: a wavefront for each tile of 16 columns, all parts one after the other.
+// Joins the parts of an item: a workgroup for a quarter of the output rows of a tile of 16 columns.  Its wavefronts take the
+// parts in turn, eight requests under way, and join.
+constexpr int kMergeSplit = 4, kMergeBatch = 8;
+
 template <typename Tag, int D, int NT>
-__global__ __launch_bounds__(64) void attend_pages_merge_kernel(PageTable t, AttendPlan plan, int max_rows, int n_q_heads,
-                                                                const int2 *__restrict__ meta, const Image<D, NT> *__restrict__ partials,
-                                                                void *__restrict__ out, float *__restrict__ lse_out) {
-  constexpr int DT = D / 16;
-  const int item = blockIdx.x / NT, nt = blockIdx.x % NT, h = blockIdx.y;
+__global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(PageTable t, AttendPlan plan, int max_rows, int n_q_heads,
+                                                                            const int2 *__restrict__ meta,
+                                                                            const Image<D, NT> *__restrict__ partials,
+                                                                            void *__restrict__ out, float *__restrict__ lse_out) {
+  constexpr int DT = D / 16 / kMergeSplit;
+  __shared__ f32x4 s_o[kAttendWaves - 1][DT][64];
+  __shared__ float s_ref[kAttendWaves][16], s_sum[kAttendWaves][16];
+  const int item = blockIdx.x / (NT * kMergeSplit), nt = blockIdx.x / kMergeSplit % NT, quarter = blockIdx.x % kMergeSplit;
+  const int h = blockIdx.y;
   const int2 m = meta[item];
   if (m.y <= 1) return;
-  const int lane = threadIdx.x, n = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const Image<D, NT> *im = partials + static_cast<int64_t>(h) * 2 * plan.target_parts + m.x;
+  float ref = -INFINITY, sum = 0.f;
+  f32x4 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0, 0, 0, 0};
+  for (int p0 = wave; p0 < m.y; p0 += kAttendWaves * kMergeBatch) {
+    float refs[kMergeBatch], sums[kMergeBatch];
+    f32x4 x[kMergeBatch][DT];
+#pragma unroll
+    for (int u = 0; u < kMergeBatch; ++u) {
+      const int p = p0 + u * kAttendWaves;
+      refs[u] = -INFINITY;
+      sums[u] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) x[u][dt] = f32x4{0, 0, 0, 0};
+      if (p < m.y) {
+        refs[u] = im[p].ref[nt][n];
+        sums[u] = im[p].sum[nt][n];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) x[u][dt] = im[p].o[(quarter * DT + dt) * NT + nt][lane];
+      }
+    }
+    float top = ref;
+#pragma unroll
+    for (int u = 0; u < kMergeBatch; ++u) top = fmaxf(top, refs[u]);
+    const float a = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top);
+    ref = top;
+    sum *= a;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[dt][e] *= a;
+#pragma unroll
+    for (int u = 0; u < kMergeBatch; ++u) {
+      const float b = refs[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(refs[u] - top);
+      sum = fmaf(sums[u], b, sum);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(x[u][dt][e], b, o[dt][e]);
+    }
+  }
+  if (g == 0) s_ref[wave][n] = ref, s_sum[wave][n] = sum;
+  if (wave > 0)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) s_o[wave - 1][dt][lane] = o[dt];
+  __syncthreads();
+  if (wave > 0) return;
+  float top = ref;
+#pragma unroll
+  for (int w = 1; w < kAttendWaves; ++w) top = fmaxf(top, s_ref[w][n]);
+  const float a = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top);
+  sum *= a;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[dt][e] *= a;
+#pragma unroll
+  for (int w = 1; w < kAttendWaves; ++w) {
+    const float b = s_ref[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_ref[w][n] - top);
+    sum = fmaf(s_sum[w][n], b, sum);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const f32x4 x = s_o[w - 1][dt][lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(x[e], b, o[dt][e]);
+    }
+  }
   int lo, hi;
   rows_of(t, item / plan.n_blocks, lo, hi);
   hi = min(hi, lo + max_rows);
   const int c = (item % plan.n_blocks) * plan.columns + nt * 16 + n;
   const int r = lo + c / plan.group;
-  const Image<D, NT> *im = partials + static_cast<int64_t>(h) * 2 * plan.target_parts + m.x;
-  float ref = -INFINITY;
-  for (int p = 0; p < m.y; ++p) ref = fmaxf(ref, im[p].ref[nt][n]);
-  f32x4 o[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0, 0, 0, 0};
-  float sum = 0.f;
-  for (int p = 0; p < m.y; ++p) {
-    const float other = im[p].ref[nt][n];
-    const float b = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - ref);
-    sum += im[p].sum[nt][n] * b;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const f32x4 x = im[p].o[dt * NT + nt][lane];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(x[e], b, o[dt][e]);
-    }
-  }
-  if (r < hi) write_columns<Tag, D>(out, lse_out, static_cast<int64_t>(r) * n_q_heads + h * plan.group + c % plan.group, g, o, 1, ref, sum);
+  if (r < hi)
+    write_columns<Tag, D, DT>(out, quarter == 0 ? lse_out : nullptr, static_cast<int64_t>(r) * n_q_heads + h * plan.group + c % plan.group,
+                              quarter * DT, g, o, 1, top, sum);
 }
 
 // Workgroups that a launch is cut into, about: four times what the chip holds at two a CU, so that uneven parts even out.
@@ -441,7 +502,8 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
     if (e != hipSuccess) return e;
   }
   if (!cut) return hipSuccess;
-  hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, NT>), dim3(static_cast<unsigned>(items * NT), d.n_kv_heads), dim3(64), 0, ctx->stream, t,
+  hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, NT>), dim3(static_cast<unsigned>(items * NT * kMergeSplit), d.n_kv_heads),
+                     dim3(kAttendThreads), 0, ctx->stream, t,
                      plan, max_rows, d.n_q_heads, meta, partials, out, lse_out);
   return hipGetLastError();
 }
