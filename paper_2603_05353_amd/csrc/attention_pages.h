@@ -136,6 +136,12 @@ __device__ __forceinline__ bool find_part(const PageTable &t, const AttendPlan &
     part.last = min(pages, part.first + step);
     if (writes_meta && mem.found[1] == 0 && tid == 0) meta[item] = make_int2(part.slot, part.n_parts);
   }
+  // the same in every lane: scalars
+  item = __builtin_amdgcn_readfirstlane(item);
+  part.first = __builtin_amdgcn_readfirstlane(part.first);
+  part.last = __builtin_amdgcn_readfirstlane(part.last);
+  part.n_parts = __builtin_amdgcn_readfirstlane(part.n_parts);
+  part.slot = __builtin_amdgcn_readfirstlane(part.slot);
   part.seq = item / plan.n_blocks;
   part.block = item - part.seq * plan.n_blocks;
   rows_of(t, part.seq, part.lo, part.hi);
@@ -154,15 +160,17 @@ __device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b, float scale) {
 // x as the sum of PARTS bf16 numbers, each the rest rounded to nearest even.
 template <int PARTS>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[PARTS]) {
-  float rest[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) rest[e] = x[e];
+  for (int e = 0; e < 8; e += 2) {
+    float a = x[e], b = x[e + 1];
 #pragma unroll
-  for (int p = 0; p < PARTS; ++p) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      out[p][e] = static_cast<__bf16>(rest[e]);
-      if (p + 1 < PARTS) rest[e] -= static_cast<float>(out[p][e]);
+    for (int p = 0; p < PARTS; ++p) {
+      const bf16x2 pair = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+      out[p][e] = pair[0];
+      out[p][e + 1] = pair[1];
+      const uint32_t w = __builtin_bit_cast(uint32_t, pair);
+      a -= __uint_as_float(w << 16);
+      b -= __uint_as_float(w & 0xFFFF0000u);
     }
   }
 }

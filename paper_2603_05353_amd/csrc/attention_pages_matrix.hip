@@ -11,6 +11,7 @@
 #include <algorithm>
 
 #include "attention_pages.h"
+#include "lds_dma.h"
 
 namespace ifkv {
 
@@ -23,22 +24,16 @@ constexpr float kLowest = -3.402823466e38f;
 // 2^(kSlack + 31), and most pages need no look at the other lanes' maxima.
 constexpr float kSlack = 16.f;
 
+// bf16 numbers that hold a query element.
 template <typename Tag>
-struct Precision;
+constexpr int kQueryParts = 3;
 template <>
-struct Precision<BF16Tag> {
-  static constexpr int kQ = 1, kP = 2;  // bf16 numbers that hold a query element and a probability
-};
-template <>
-struct Precision<F32Tag> {
-  static constexpr int kQ = 3, kP = 3;
-};
+constexpr int kQueryParts<BF16Tag> = 1;
 
-// Partial results of one part: accumulators as the wavefront holds them, then reference and sum of every column.
+// Partial results of one part: accumulators as the wavefronts hold them, then reference and sum of every column.
 template <int D, int NT>
 struct Image {
-  static constexpr int kRegs = NT * D / 16;       // f32x4 of a lane
-  f32x4 o[kRegs][64];
+  f32x4 o[NT * D / 16][64];
   float ref[NT][16], sum[NT][16];
 };
 
@@ -65,86 +60,305 @@ __device__ __forceinline__ void write_columns(void *out, float *lse_out, int64_t
   if (lse_out != nullptr && g == 0) lse_out[row_head] = ref == -INFINITY ? -INFINITY : ref * kLn2 + logf(sum);
 }
 
-// ---------------------------------------------------------------------------
-// A workgroup's four wavefronts take the pages of a part in turn, all for the same NT * 16 query columns, and join at the end.
-// ---------------------------------------------------------------------------
-template <typename Tag, int D, int NT>
-__global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_pages_kernel(
-    PageTable t, AttendPlan plan, int max_rows, const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages,
-    const float *__restrict__ k_scale, const float *__restrict__ v_scale, int n_pages, int n_q_heads, int n_kv_heads, float logit_scale,
-    const void *__restrict__ q, int64_t q_stride, void *__restrict__ out, float *__restrict__ lse_out, int2 *__restrict__ meta,
-    Image<D, NT> *__restrict__ partials) {
-  constexpr int QP = Precision<Tag>::kQ, PP = Precision<Tag>::kP;
-  constexpr int KS = D / 32;       // steps of the first product
-  constexpr int KV = D / 64;       // 16-byte key loads of a lane and block of 16 tokens
-  constexpr int DT = D / 16;       // blocks of 16 output rows
-  constexpr int TILE = kPageTokens * D;
-  __shared__ union {
-    AttendPlanMemory plan;
-    Image<D, NT> image[2];
-  } mem;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n = lane & 15, g = lane >> 4;
-  const int h = blockIdx.y;
-  AttendPart part;
-  if (!find_part(t, plan, max_rows, blockIdx.x, h == 0, meta, mem.plan, part)) return;
+// What a lane names of a page: bytes from the page's start (of its kv head) of the rt-th block of 16 tokens' u-th 16 bytes of keys,
+// and of the dt-th block of 16 value rows.
+template <int D>
+__device__ __forceinline__ int key_offset(int lane, int rt, int u) {
+  return (rt * 16 + (lane & 15)) * D + (lane >> 4) * (D / 4) + u * 16;
+}
+__device__ __forceinline__ int value_offset(int lane, int dt) { return (dt * 16 + (lane & 15)) * kPageTokens + (lane >> 4) * 16; }
 
-  // this lane's column of every tile: its row and where it is in out; columns that see nothing get queries of zero, no
-  // mask, and at the end zeros
-  const int grp = plan.group;
-  int pos[NT];
-  int64_t row_head[NT];
-  bool real[NT];   // a row of the sequence
-  bf16x8 qf[NT][QP][KS];
-  int lowest = INT32_MAX;
+// NT * 16 query columns of a wavefront and what it has added up for them.  Lane l holds column l % 16 of every tile; the four
+// lanes of a column share its reference, each has its own tokens' sum.
+template <typename Tag, int D, int NT, int PP>
+struct Columns {
+  static constexpr int QP = kQueryParts<Tag>;
+  static constexpr int KS = D / 32;       // steps of the first product
+  static constexpr int KV = D / 64;       // 16-byte key loads of a lane and block of 16 tokens
+  static constexpr int DT = D / 16;       // blocks of 16 output rows
+  bf16x8 q[NT][QP][KS];
+  f32x4 o[DT][NT];
+  float ref[NT], neg_ref[NT], sum[NT];
+  int pos[NT];          // INT32_MAX: sees nothing
+  int64_t row_head[NT]; // -1: no row
+  int lowest, highest;  // positions of the wavefront's columns that see something (INT32_MAX and -1: none does)
+  int n, g;
+
+  // columns first_column .. of the sequence's
+  __device__ __forceinline__ void start(const PageTable &t, const AttendPart &part, int first_column, int grp, int h, int n_q_heads,
+                                        const void *queries, int64_t q_stride) {
+    const int lane = threadIdx.x & 63;
+    n = lane & 15;
+    g = lane >> 4;
+    lowest = INT32_MAX;
+    highest = -1;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int c = part.block * plan.columns + nt * 16 + n;
-    const int r = part.lo + c / grp;
-    const int hq = h * grp + c % grp;
-    real[nt] = r < part.hi;
-    pos[nt] = real[nt] ? t.row_pos[r] : -1;
-    row_head[nt] = static_cast<int64_t>(r) * n_q_heads + hq;
-    const bool sees = pos[nt] >= 0 && (pos[nt] >> 6) < t.width;
-    if (!sees) pos[nt] = INT32_MAX;
-    lowest = min(lowest, pos[nt]);
-    const char *src = static_cast<const char *>(q) + (r * q_stride + static_cast<int64_t>(hq) * D + g * (D / 4)) * Elem<Tag>::kBytes;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int c = first_column + nt * 16 + n;
+      const int r = part.lo + c / grp;
+      const int hq = h * grp + c % grp;
+      const bool real = r < part.hi;
+      pos[nt] = real ? t.row_pos[r] : -1;
+      row_head[nt] = real ? static_cast<int64_t>(r) * n_q_heads + hq : -1;
+      const bool sees = pos[nt] >= 0 && (pos[nt] >> 6) < t.width;
+      if (sees) highest = max(highest, pos[nt]);
+      if (!sees) pos[nt] = INT32_MAX;
+      lowest = min(lowest, pos[nt]);
+      const char *src = static_cast<const char *>(queries) + (r * q_stride + static_cast<int64_t>(hq) * D + g * (D / 4)) * Elem<Tag>::kBytes;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      if constexpr (QP == 1) {
-        v4u w = {0, 0, 0, 0};
-        if (sees) w = reinterpret_cast<const v4u *>(src)[ks];
-        qf[nt][0][ks] = __builtin_bit_cast(bf16x8, w);
-      } else {
-        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (sees) {
-          *reinterpret_cast<f32x4 *>(x) = reinterpret_cast<const f32x4 *>(src)[2 * ks];
-          *reinterpret_cast<f32x4 *>(x + 4) = reinterpret_cast<const f32x4 *>(src)[2 * ks + 1];
+      for (int ks = 0; ks < KS; ++ks) {
+        if constexpr (QP == 1) {
+          v4u w = {0, 0, 0, 0};
+          if (sees) w = reinterpret_cast<const v4u *>(src)[ks];
+          q[nt][0][ks] = __builtin_bit_cast(bf16x8, w);
+        } else {
+          float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          if (sees) {
+            *reinterpret_cast<f32x4 *>(x) = reinterpret_cast<const f32x4 *>(src)[2 * ks];
+            *reinterpret_cast<f32x4 *>(x + 4) = reinterpret_cast<const f32x4 *>(src)[2 * ks + 1];
+          }
+          bf16x8 s[QP];
+          split8<QP>(x, s);
+#pragma unroll
+          for (int p = 0; p < QP; ++p) {
+            q[nt][p][ks] = s[p];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (p > 0 && !(fabsf(x[e]) < INFINITY)) q[nt][p][ks][e] = static_cast<__bf16>(0.f);
+          }
         }
-        bf16x8 s[QP];
-        split8<QP>(x, s);
+      }
+      ref[nt] = -INFINITY;
+      neg_ref[nt] = 0.f;
+      sum[nt] = 0.f;
 #pragma unroll
-        for (int p = 0; p < QP; ++p) {
-          qf[nt][p][ks] = s[p];
+      for (int dt = 0; dt < DT; ++dt) o[dt][nt] = f32x4{0, 0, 0, 0};
+    }
+    lowest = __builtin_amdgcn_readfirstlane(wave_min_i(lowest));
+    highest = __builtin_amdgcn_readfirstlane(wave_max_i(highest));
+  }
+
+  // keys(rt, u): what this lane names of a page (key_offset)
+  template <typename F>
+  __device__ __forceinline__ void logits(F keys, float scale, f32x4 (&s)[4][NT]) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (p > 0 && !(fabsf(x[e]) < INFINITY)) qf[nt][p][ks][e] = static_cast<__bf16>(0.f);
+    for (int rt = 0; rt < 4; ++rt) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s[rt][nt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int u = 0; u < KV; ++u) {
+        const v4u w = keys(rt, u);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const bf16x8 a = half == 0 ? widen(w.x, w.y, scale) : widen(w.z, w.w, scale);
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p)   // smallest first
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              s[rt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nt][p][2 * u + half], s[rt][nt], 0, 0, 0);
         }
       }
     }
   }
-  const int min_pos = wave_min_i(lowest);
 
-  f32x4 o[DT][NT];
-  float ref[NT], neg_ref[NT], sum[NT];
+  __device__ __forceinline__ bool masked(int token0) const { return token0 + kPageTokens - 1 > lowest; }
+
+  // exponentials of a page's logits, as the second product takes them
+  __device__ __forceinline__ void weights(int token0, float logit_scale, f32x4 (&s)[4][NT], bf16x8 (&w)[2][NT][PP]) {
+    if (masked(token0)) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    ref[nt] = -INFINITY;
-    neg_ref[nt] = 0.f;
-    sum[nt] = 0.f;
+      for (int nt = 0; nt < NT; ++nt) {
+        const int last = pos[nt] - token0 - g * 4;   // of the page's tokens, from the lane's first on
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt][nt] = f32x4{0, 0, 0, 0};
+        for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[rt][nt][e] = rt * 16 + e > last ? -INFINITY : s[rt][nt][e];
+      }
+    }
+    bool rise = false;
+    float top[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, s[rt][nt][e]);
+      top[nt] = m * logit_scale;
+      rise = rise || ref[nt] == -INFINITY || top[nt] > ref[nt] + kSlack;
+    }
+    if (__ballot(rise) != 0) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float m = top[nt];
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float old = ref[nt];
+        if (token0 <= pos[nt]) ref[nt] = fmaxf(old, fmaxf(m, kLowest));
+        neg_ref[nt] = ref[nt] == -INFINITY ? 0.f : -ref[nt];
+        const float by = old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(old - ref[nt]);
+        sum[nt] *= by;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[dt][nt][e] *= by;
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(s[2 * st + e / 4][nt][e % 4], logit_scale, neg_ref[nt]));
+          sum[nt] += p[e];
+        }
+        split8<PP>(p, w[st][nt]);
+      }
+    }
   }
+
+  // the bytes that are NaN, 1 in each
+  static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7; }
+
+  // Values behind a column's token count nothing, NaN neither.  Where a page that has such tokens holds NaN at all, its NaN
+  // bytes are taken as zero by add_values (the answer is true), and columns that do see one become NaN here.
+  template <typename F>
+  __device__ __forceinline__ bool drop_nan(int token0, F values) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const v4u v = values(dt);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F7F7F7Fu) + 0x01010101u;
+      if (dt % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    if (__ballot((any & 0x80808080u) != 0) == 0) return false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int last = pos[nt] - token0 - g * 4;
+      bf16x8 seen[2];
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) seen[st][e] = static_cast<__bf16>((2 * st + e / 4) * 16 + e % 4 <= last ? 1.f : 0.f);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const v4u v = values(dt);
+        v4u one;   // 1.0 in e4m3 where there is a NaN
+#pragma unroll
+        for (int e = 0; e < 4; ++e) one[e] = nan_bytes(v[e]) * 0x38u;
+        f32x4 count = {0, 0, 0, 0};
+        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(one.x, one.y, 1.f), seen[0], count, 0, 0, 0);
+        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(one.z, one.w, 1.f), seen[1], count, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (count[e] > 0.f) o[dt][nt][e] = __uint_as_float(0x7FC00000u);
+        __builtin_amdgcn_sched_barrier(0);   // one after the other: this path must not take registers from the others
+      }
+    }
+    return true;
+  }
+
+  template <bool CLEAN, typename F>
+  __device__ __forceinline__ void add(F values, float scale, const bf16x8 (&w)[2][NT][PP]) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      v4u v = values(dt);
+      if constexpr (CLEAN)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] &= ~(nan_bytes(v[e]) * 0xFFu);
+      const bf16x8 a0 = widen(v.x, v.y, scale), a1 = widen(v.z, v.w, scale);
+#pragma unroll
+      for (int p = PP - 1; p >= 0; --p)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w[0][nt][p], o[dt][nt], 0, 0, 0);
+          o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w[1][nt][p], o[dt][nt], 0, 0, 0);
+        }
+      if (CLEAN || dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // values(dt): what this lane names of a page (value_offset)
+  template <typename F>
+  __device__ __forceinline__ void add_values(int token0, F values, float scale, const bf16x8 (&w)[2][NT][PP]) {
+    if (masked(token0) && drop_nan(token0, values))
+      add<true>(values, scale, w);
+    else
+      add<false>(values, scale, w);
+  }
+
+  // a column's tokens are spread over four lanes
+  __device__ __forceinline__ void join_sums() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      sum[nt] += __shfl_xor(sum[nt], 16, 64);
+      sum[nt] += __shfl_xor(sum[nt], 32, 64);
+    }
+  }
+
+  // into an image of TILES tiles, as tiles from first on
+  template <int TILES>
+  __device__ __forceinline__ void save(Image<D, TILES> &im, int first) const {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) im.o[dt * TILES + first + nt][g * 16 + n] = o[dt][nt];
+      if (g == 0) im.ref[first + nt][n] = ref[nt], im.sum[first + nt][n] = sum[nt];
+    }
+  }
+
+  __device__ __forceinline__ void finish(void *out, float *lse_out) const {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      if (row_head[nt] >= 0) write_columns<Tag, D, DT>(out, lse_out, row_head[nt], 0, g, &o[0][nt], NT, ref[nt], sum[nt]);
+  }
+
+  // columns that see nothing had queries of zero and no mask
+  __device__ __forceinline__ void forget_unseen() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      if (pos[nt] == INT32_MAX) ref[nt] = -INFINITY;
+  }
+};
+
+struct AttendArgs {
+  PageTable t;
+  AttendPlan plan;
+  const uint8_t *k_pages, *v_pages;
+  const float *k_scale, *v_scale;
+  const void *q;
+  void *out;
+  float *lse_out;
+  int2 *meta;
+  int64_t q_stride;
+  int max_rows, n_pages, n_q_heads, n_kv_heads;
+  float logit_scale;
+};
+
+// ---------------------------------------------------------------------------
+// Up to 16 query columns a sequence: a workgroup's four wavefronts take the pages of a part in turn and join at the end.
+// ---------------------------------------------------------------------------
+// (the operands of an fp32 layer with heads of 128 need more registers than two wavefronts a SIMD leave)
+template <typename Tag, int D>
+constexpr int kFewWaves = kQueryParts<Tag> == 3 && D == 128 ? 1 : 2;
+
+template <typename Tag, int D>
+__global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D>)) void attend_pages_kernel(AttendArgs a, Image<D, 1> *__restrict__ partials) {
+  constexpr int PP = kQueryParts<Tag> == 1 ? 2 : 3;
+  using Cols = Columns<Tag, D, 1, PP>;
+  constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
+  __shared__ union {
+    AttendPlanMemory plan;
+    Image<D, 1> image[2];
+  } mem;
+  const PageTable &t = a.t;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
+  AttendPart part;
+  if (!find_part(t, a.plan, a.max_rows, blockIdx.x, h == 0, a.meta, mem.plan, part)) return;
+  Cols c;
+  c.start(t, part, part.block * a.plan.columns, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
 
   const int32_t *row_of_table = t.table + static_cast<int64_t>(part.seq) * t.width;
   // pages of this wavefront, 64 at a time: lane i knows the i-th
@@ -152,218 +366,171 @@ __global__ __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) void attend_pages_
     const int mine = base + lane * kAttendWaves;
     int entry = -1;
     if (mine < part.last) entry = row_of_table[mine];
-    uint64_t todo = __ballot(entry >= 0 && entry < n_pages);
+    uint64_t todo = __ballot(entry >= 0 && entry < a.n_pages);
     if (todo == 0) continue;
     float ks_lane = 1.f, vs_lane = 1.f;
-    if (entry >= 0 && entry < n_pages) {
-      const int64_t at = static_cast<int64_t>(entry) * n_kv_heads + h;
-      ks_lane = k_scale[at];
-      vs_lane = v_scale[at];
+    if (entry >= 0 && entry < a.n_pages) {
+      const int64_t at = static_cast<int64_t>(entry) * a.n_kv_heads + h;
+      ks_lane = a.k_scale[at];
+      vs_lane = a.v_scale[at];
     }
     v4u kb[4][KV], vb[DT];
     auto page_at = [&](int i) __attribute__((always_inline)) {
-      return (static_cast<int64_t>(__builtin_amdgcn_readlane(entry, i)) * n_kv_heads + h) * TILE;
+      return (static_cast<int64_t>(__builtin_amdgcn_readlane(entry, i)) * a.n_kv_heads + h) * TILE;
     };
     auto load_k = [&](int64_t at) __attribute__((always_inline)) {
-      const uint8_t *src = k_pages + at + n * D + g * (D / 4);
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
-        for (int u = 0; u < KV; ++u) kb[rt][u] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(src + rt * 16 * D + u * 16));
+        for (int u = 0; u < KV; ++u)
+          kb[rt][u] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(a.k_pages + at + key_offset<D>(lane, rt, u)));
     };
     auto load_v = [&](int64_t at) __attribute__((always_inline)) {
-      const uint8_t *src = v_pages + at + n * kPageTokens + g * 16;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) vb[dt] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(src + dt * 16 * kPageTokens));
+      for (int dt = 0; dt < DT; ++dt) vb[dt] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(a.v_pages + at + value_offset(lane, dt)));
     };
     int i = __builtin_ctzll(todo);
-    {
-      const int64_t at = page_at(i);
-      load_k(at);
-      load_v(at);
-    }
+    load_k(page_at(i));
+    load_v(page_at(i));
     while (todo != 0) {
       todo &= todo - 1;
-      const int next = todo != 0 ? __builtin_ctzll(todo) : i;   // (the last page is requested once more, from the cache)
+      const int next = todo != 0 ? __builtin_ctzll(todo) : i;
       const int64_t next_at = page_at(next);
       const float ks_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_lane), i));
       const float vs_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_lane), i));
       const int token0 = (base + i * kAttendWaves) * kPageTokens;
-
-      f32x4 s[4][NT];
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[rt][nt] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const v4u w = kb[rt][ks / 2];
-          const bf16x8 a = ks % 2 == 0 ? widen(w.x, w.y, ks_page) : widen(w.z, w.w, ks_page);
-#pragma unroll
-          for (int p = QP - 1; p >= 0; --p)   // smallest first
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[rt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[nt][p][ks], s[rt][nt], 0, 0, 0);
-        }
-      }
+      f32x4 s[4][1];
+      c.logits([&](int rt, int u) __attribute__((always_inline)) { return kb[rt][u]; }, ks_page, s);
+      __builtin_amdgcn_sched_barrier(0);
       if (next != i) load_k(next_at);
-
-      const bool masked = token0 + kPageTokens - 1 > min_pos;
-      if (masked) {
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (token0 + rt * 16 + g * 4 + e > pos[nt]) s[rt][nt][e] = -INFINITY;
-      }
-      bool rise = false;
-      float top[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float m = -INFINITY;
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) m = fmaxf(m, s[rt][nt][e]);
-        top[nt] = m * logit_scale;
-        rise = rise || ref[nt] == -INFINITY || top[nt] > ref[nt] + kSlack;
-      }
-      if (__ballot(rise) != 0) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float m = top[nt];
-          m = fmaxf(m, __shfl_xor(m, 16, 64));
-          m = fmaxf(m, __shfl_xor(m, 32, 64));
-          const float old = ref[nt];
-          if (token0 <= pos[nt]) ref[nt] = fmaxf(old, fmaxf(m, kLowest));
-          neg_ref[nt] = ref[nt] == -INFINITY ? 0.f : -ref[nt];
-          const float by = old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(old - ref[nt]);
-          sum[nt] *= by;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[dt][nt][e] *= by;
-        }
-      }
-      bf16x8 pf[2][NT][PP];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          float p[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(fmaf(s[2 * st + e / 4][nt][e % 4], logit_scale, neg_ref[nt]));
-            sum[nt] += p[e];
-          }
-          split8<PP>(p, pf[st][nt]);
-        }
-      }
-      if (masked) {
-        // Values behind a column's token count nothing, NaN neither: NaN bytes become zero, and columns that do see one get it back.
-        bool any = false;
-        v4u spoiled[DT];
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t w = vb[dt][e];
-            const uint32_t bad = (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;   // 1 in the bytes that are NaN
-            any = any || bad != 0;
-            spoiled[dt][e] = bad * 0x38u;                                                   // 1.0 in e4m3
-            vb[dt][e] = w & ~(bad * 0xFFu);
-          }
-        }
-        if (__ballot(any) != 0) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            bf16x8 seen[2];
-#pragma unroll
-            for (int st = 0; st < 2; ++st)
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                seen[st][e] = static_cast<__bf16>(token0 + (2 * st + e / 4) * 16 + g * 4 + e % 4 <= pos[nt] ? 1.f : 0.f);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-              f32x4 count = {0, 0, 0, 0};
-              count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(spoiled[dt].x, spoiled[dt].y, 1.f), seen[0], count, 0, 0, 0);
-              count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(spoiled[dt].z, spoiled[dt].w, 1.f), seen[1], count, 0, 0, 0);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (count[e] > 0.f) o[dt][nt][e] = __uint_as_float(0x7FC00000u);
-            }
-          }
-        }
-      }
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const bf16x8 a0 = widen(vb[dt].x, vb[dt].y, vs_page), a1 = widen(vb[dt].z, vb[dt].w, vs_page);
-#pragma unroll
-        for (int p = PP - 1; p >= 0; --p)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, pf[0][nt][p], o[dt][nt], 0, 0, 0);
-            o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, pf[1][nt][p], o[dt][nt], 0, 0, 0);
-          }
-      }
+      bf16x8 w[2][1][PP];
+      c.weights(token0, a.logit_scale, s, w);
+      __builtin_amdgcn_sched_barrier(0);
+      c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return vb[dt]; }, vs_page, w);
       if (next != i) load_v(next_at);
       i = next;
     }
   }
-
-  // a column's tokens are spread over four lanes
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    sum[nt] += __shfl_xor(sum[nt], 16, 64);
-    sum[nt] += __shfl_xor(sum[nt], 32, 64);
-  }
+  c.join_sums();
   // wavefronts 2 and 3 into 0 and 1, then 1 into 0
 #pragma unroll
   for (int half = 2; half >= 1; half >>= 1) {
     __syncthreads();   // (the plan's memory, or the images of the step before)
-    if (wave >= half && wave < 2 * half) {
-      Image<D, NT> &im = mem.image[wave - half];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) im.o[dt * NT + nt][lane] = o[dt][nt];
-        if (g == 0) im.ref[nt][n] = ref[nt], im.sum[nt][n] = sum[nt];
-      }
-    }
+    if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
     __syncthreads();
     if (wave < half) {
-      const Image<D, NT> &im = mem.image[wave];
+      const Image<D, 1> &im = mem.image[wave];
+      const float other = im.ref[0][c.n], m = fmaxf(c.ref[0], other);
+      const float x = c.ref[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[0] - m);
+      const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
+      c.ref[0] = m;
+      c.sum[0] = c.sum[0] * x + im.sum[0][c.n] * y;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float other = im.ref[nt][n], m = fmaxf(ref[nt], other);
-        const float a = ref[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[nt] - m);
-        const float b = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
-        ref[nt] = m;
-        sum[nt] = sum[nt] * a + im.sum[nt][n] * b;
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 o = im.o[dt][lane];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const f32x4 x = im.o[dt * NT + nt][lane];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[dt][nt][e] = o[dt][nt][e] * a + x[e] * b;
-        }
+        for (int e = 0; e < 4; ++e) c.o[dt][0][e] = c.o[dt][0][e] * x + o[e] * y;
       }
     }
   }
   if (wave != 0) return;
-  if (part.n_parts == 1) {
+  c.forget_unseen();
+  if (part.n_parts == 1)
+    c.finish(a.out, a.lse_out);
+  else
+    c.save(partials[static_cast<int64_t>(h) * 2 * a.plan.target_parts + part.slot], 0);
+}
+
+// ---------------------------------------------------------------------------
+// More columns: each of the four wavefronts has NT * 16 of its own and all of them go through the same pages, which direct
+// loads bring into LDS kStages - 1 ahead, in the order in which the lanes take them out again (no bank is asked twice).
+// ---------------------------------------------------------------------------
+constexpr int kStages = 4;
+constexpr int kPageList = kAttendThreads;   // pages whose places are looked up together
+
+template <typename Tag, int D, int NT, int PP>
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(AttendArgs a, Image<D, 4 * NT> *__restrict__ partials) {
+  using Cols = Columns<Tag, D, NT, PP>;
+  constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
+  constexpr int LOADS = 2 * TILE / 1024;              // of 1 KiB, a page: keys first
+  constexpr int MINE = LOADS / kAttendWaves;          // of a wavefront
+  __shared__ v4u s_stage[kStages][LOADS][64];
+  __shared__ union {
+    AttendPlanMemory plan;
+    struct {
+      int4 entry[kPageList];                          // page, its place in the sequence, scales
+      int count[kAttendWaves];
+    } list;
+  } mem;
+  const PageTable &t = a.t;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = blockIdx.y;
+  AttendPart part;
+  if (!find_part(t, a.plan, a.max_rows, blockIdx.x, h == 0, a.meta, mem.plan, part)) return;
+  Cols c;
+  c.start(t, part, part.block * a.plan.columns + wave * NT * 16, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
+
+  const int32_t *row_of_table = t.table + static_cast<int64_t>(part.seq) * t.width;
+  int offset[MINE];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-      if (real[nt]) write_columns<Tag, D, DT>(out, lse_out, row_head[nt], 0, g, &o[0][nt], NT, pos[nt] == INT32_MAX ? -INFINITY : ref[nt], sum[nt]);
-    return;
+  for (int u = 0; u < MINE; ++u) {
+    const int l = wave * MINE + u;
+    offset[u] = l < LOADS / 2 ? key_offset<D>(lane, l / KV, l % KV) : value_offset(lane, l - LOADS / 2);
   }
-  Image<D, NT> &im = partials[static_cast<int64_t>(h) * 2 * plan.target_parts + part.slot];
+  const uint8_t *pool = wave < kAttendWaves / 2 ? a.k_pages : a.v_pages;   // the first half of the loads are keys
+  for (int base = part.first; base < part.last; base += kPageList) {
+    __syncthreads();   // (the list before has been read, or the plan's memory)
+    int entry = -1;
+    if (base + tid < part.last) entry = row_of_table[base + tid];
+    const uint64_t there = __ballot(entry >= 0 && entry < a.n_pages);
+    if (lane == 0) mem.list.count[wave] = __builtin_popcountll(there);
+    __syncthreads();
+    int n_list = 0, at = __builtin_popcountll(there & ((1ull << lane) - 1));
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+    for (int w = 0; w < kAttendWaves; ++w) {
+      if (w < wave) at += mem.list.count[w];
+      n_list += mem.list.count[w];
+    }
+    if (entry >= 0 && entry < a.n_pages) {
+      const int64_t s = static_cast<int64_t>(entry) * a.n_kv_heads + h;
+      mem.list.entry[at] = make_int4(entry, base + tid, __float_as_int(a.k_scale[s]), __float_as_int(a.v_scale[s]));
+    }
+    __syncthreads();
+    if (n_list == 0) continue;
+    auto request = [&](int p) __attribute__((always_inline)) {   // (behind the end: the last page once more, so that counts stay the same)
+      const int page = mem.list.entry[min(p, n_list - 1)].x;
+      const uint8_t *src = pool + (static_cast<int64_t>(page) * a.n_kv_heads + h) * TILE;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) im.o[dt * NT + nt][lane] = o[dt][nt];
-    if (g == 0) im.ref[nt][n] = pos[nt] == INT32_MAX ? -INFINITY : ref[nt], im.sum[nt][n] = sum[nt];
+      for (int u = 0; u < MINE; ++u)
+        dma16(src + offset[u], lds_address(&s_stage[p % kStages][wave * MINE + u][0]));
+    };
+    wait_vmem<0>();
+#pragma unroll
+    for (int p = 0; p < kStages - 1; ++p) request(p);
+    for (int p = 0; p < n_list; ++p) {
+      wait_vmem<(kStages - 2) * MINE>();   // this wavefront's share of page p is there
+      wait_lds_reads();                    // and it has taken all it needs of page p - 1
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" : : : "memory");
+      request(p + kStages - 1);
+      const int4 e = mem.list.entry[p];
+      const int token0 = __builtin_amdgcn_readfirstlane(e.y) * kPageTokens;
+      if (token0 > c.highest) continue;
+      const v4u (*stage)[64] = s_stage[p % kStages];
+      f32x4 s[4][NT];
+      c.logits([&](int rt, int u) __attribute__((always_inline)) { return stage[rt * KV + u][lane]; }, __int_as_float(e.z), s);
+      bf16x8 w[2][NT][PP];
+      c.weights(token0, a.logit_scale, s, w);
+      __builtin_amdgcn_sched_barrier(0);
+      c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return stage[LOADS / 2 + dt][lane]; }, __int_as_float(e.w), w);
+    }
+    wait_vmem<0>();   // nothing is under way into LDS that is given up or used again
   }
+  c.join_sums();
+  c.forget_unseen();
+  if (part.n_parts == 1)
+    c.finish(a.out, a.lse_out);
+  else
+    c.save(partials[static_cast<int64_t>(h) * 2 * a.plan.target_parts + part.slot], wave * NT);
 }
 
 // Joins the parts of an item: a workgroup for a quarter of the output rows of a tile of 16 columns.  Its wavefronts take the
@@ -461,50 +628,59 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
                               quarter * DT, g, o, 1, top, sum);
 }
 
-// Workgroups that a launch is cut into, about: four times what the chip holds at two a CU, so that uneven parts even out.
-constexpr int kTargetWorkgroups = 1024;
-constexpr int kLeastPages = 8;                    // of a part: two for each wavefront
 constexpr size_t kMetaBytes = kMaxItems * sizeof(int2);
 
-template <typename Tag, int D, int NT>
-size_t scratch_for(int n_kv_heads) {
-  const int target = std::max(1, kTargetWorkgroups / NT / n_kv_heads);
-  return kMetaBytes + static_cast<size_t>(2) * target * n_kv_heads * sizeof(Image<D, NT>);
-}
+// How a launch with TILES tiles of 16 columns a workgroup is divided.
+template <int TILES>
+struct Division {
+  // Workgroups that a launch is cut into, about: decoding twice what the chip holds at two a CU, so that uneven parts even out;
+  // with more columns, whose partial results are larger, what it holds
+  static constexpr int kWorkgroups = TILES == 1 ? 1024 : 512;
+  static constexpr int kLeastPages = 8;
+  static int target_parts(int n_kv_heads) { return std::max(1, kWorkgroups / n_kv_heads); }
+  template <int D>
+  static size_t scratch_bytes(int n_kv_heads) {
+    return kMetaBytes + static_cast<size_t>(2) * target_parts(n_kv_heads) * n_kv_heads * sizeof(Image<D, TILES>);
+  }
+};
 
-template <typename Tag, int D, int NT>
+template <typename Tag, int D, int TILES>
 hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int max_rows, const void *q, int64_t q_stride, void *out,
                float *lse_out) {
   const auto &d = ctx->desc;
+  using Div = Division<TILES>;
   AttendPlan plan;
   plan.group = d.n_q_heads / d.n_kv_heads;
-  plan.columns = NT * 16;
+  plan.columns = TILES * 16;
   plan.n_blocks = static_cast<int>((static_cast<int64_t>(max_rows) * plan.group + plan.columns - 1) / plan.columns);
-  plan.least_pages = kLeastPages;
+  plan.least_pages = Div::kLeastPages;
   const int64_t items = static_cast<int64_t>(t.n_seqs) * plan.n_blocks;
-  const bool cut = t.width > kLeastPages && items <= kMaxItems && items * t.width < INT32_MAX;   // (pages are added up in 32 bits)
-  plan.target_parts = cut ? std::max(1, kTargetWorkgroups / NT / d.n_kv_heads) : 0;
+  const bool cut = t.width > Div::kLeastPages && items <= kMaxItems && items * t.width < INT32_MAX;   // (pages are added up in 32 bits)
+  plan.target_parts = cut ? Div::target_parts(d.n_kv_heads) : 0;
   int2 *meta = static_cast<int2 *>(ctx->page_partials);
-  Image<D, NT> *partials = reinterpret_cast<Image<D, NT> *>(static_cast<char *>(ctx->page_partials) + kMetaBytes);
+  Image<D, TILES> *partials = reinterpret_cast<Image<D, TILES> *>(static_cast<char *>(ctx->page_partials) + kMetaBytes);
   // a grid has fewer than 2^32 threads: so many sequences a launch (all of them where items are cut)
   const int step = std::max(1, (1 << 23) / plan.n_blocks);
   for (int s = 0; s < t.n_seqs; s += step) {
-    const PageTable u = t.from(s, std::min(step, t.n_seqs - s));
     const int64_t skip = t.row_start != nullptr ? 0 : s;  // rows of the sequences before, where each has one
-    const int64_t n_items = static_cast<int64_t>(u.n_seqs) * plan.n_blocks;
-    hipLaunchKernelGGL((attend_pages_kernel<Tag, D, NT>), dim3(static_cast<unsigned>(n_items + plan.target_parts), d.n_kv_heads),
-                       dim3(kAttendThreads), 0, ctx->stream, u, plan, max_rows, static_cast<const uint8_t *>(pages.k),
-                       static_cast<const uint8_t *>(pages.v), pages.k_scale, pages.v_scale, static_cast<int>(pages.n_pages), d.n_q_heads,
-                       d.n_kv_heads, ctx->sm_scale * kLog2e, static_cast<const char *>(q) + skip * q_stride * Elem<Tag>::kBytes, q_stride,
-                       static_cast<char *>(out) + skip * d.n_q_heads * D * Elem<Tag>::kBytes,
-                       lse_out != nullptr ? lse_out + skip * d.n_q_heads : nullptr, meta, partials);
+    const AttendArgs a = {t.from(s, std::min(step, t.n_seqs - s)), plan, static_cast<const uint8_t *>(pages.k),
+                          static_cast<const uint8_t *>(pages.v), pages.k_scale, pages.v_scale,
+                          static_cast<const char *>(q) + skip * q_stride * Elem<Tag>::kBytes,
+                          static_cast<char *>(out) + skip * d.n_q_heads * D * Elem<Tag>::kBytes,
+                          lse_out != nullptr ? lse_out + skip * d.n_q_heads : nullptr, meta, q_stride, max_rows,
+                          static_cast<int>(pages.n_pages), d.n_q_heads, d.n_kv_heads, ctx->sm_scale * kLog2e};
+    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.t.n_seqs) * plan.n_blocks + plan.target_parts), d.n_kv_heads), block(kAttendThreads);
+    if constexpr (TILES == 1)
+      hipLaunchKernelGGL((attend_pages_kernel<Tag, D>), grid, block, 0, ctx->stream, a, partials);
+    else
+      hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, kQueryParts<Tag> == 1 ? (TILES == 4 ? 2 : 1) : 3>), grid, block, 0,
+                         ctx->stream, a, partials);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (!cut) return hipSuccess;
-  hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, NT>), dim3(static_cast<unsigned>(items * NT * kMergeSplit), d.n_kv_heads),
-                     dim3(kAttendThreads), 0, ctx->stream, t,
-                     plan, max_rows, d.n_q_heads, meta, partials, out, lse_out);
+  hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, TILES>), dim3(static_cast<unsigned>(items * TILES * kMergeSplit), d.n_kv_heads),
+                     dim3(kAttendThreads), 0, ctx->stream, t, plan, max_rows, d.n_q_heads, meta, partials, out, lse_out);
   return hipGetLastError();
 }
 
@@ -513,21 +689,21 @@ hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTa
                        void *out, float *lse_out) {
   const int64_t columns = static_cast<int64_t>(max_rows) * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads);
   if (columns <= 16) return run<Tag, D, 1>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
-  if (columns <= 32 || Precision<Tag>::kQ > 1) return run<Tag, D, 2>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
-  if constexpr (Precision<Tag>::kQ == 1) return run<Tag, D, 4>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+  if (columns <= 64 || kQueryParts<Tag> > 1) return run<Tag, D, 4>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+  if constexpr (kQueryParts<Tag> == 1) return run<Tag, D, 8>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+}
+
+template <int D>
+size_t scratch_bytes(int n_kv_heads, bool bf16) {
+  const size_t few = std::max(Division<1>::scratch_bytes<D>(n_kv_heads), Division<4>::scratch_bytes<D>(n_kv_heads));
+  return bf16 ? std::max(few, Division<8>::scratch_bytes<D>(n_kv_heads)) : few;
 }
 
 }  // namespace
 
 size_t attend_matrix_scratch_bytes(const ifkv_ctx *ctx) {
   const auto &d = ctx->desc;
-  const bool wide = d.head_dim == 128;
-  if (d.dtype == IFKV_F32) {
-    return wide ? std::max(scratch_for<F32Tag, 128, 1>(d.n_kv_heads), scratch_for<F32Tag, 128, 2>(d.n_kv_heads))
-                : std::max(scratch_for<F32Tag, 64, 1>(d.n_kv_heads), scratch_for<F32Tag, 64, 2>(d.n_kv_heads));
-  }
-  return wide ? std::max({scratch_for<BF16Tag, 128, 1>(d.n_kv_heads), scratch_for<BF16Tag, 128, 2>(d.n_kv_heads), scratch_for<BF16Tag, 128, 4>(d.n_kv_heads)})
-              : std::max({scratch_for<BF16Tag, 64, 1>(d.n_kv_heads), scratch_for<BF16Tag, 64, 2>(d.n_kv_heads), scratch_for<BF16Tag, 64, 4>(d.n_kv_heads)});
+  return d.head_dim == 128 ? scratch_bytes<128>(d.n_kv_heads, d.dtype == IFKV_BF16) : scratch_bytes<64>(d.n_kv_heads, d.dtype == IFKV_BF16);
 }
 
 hipError_t launch_attend_matrix(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int32_t max_rows, const void *q,
