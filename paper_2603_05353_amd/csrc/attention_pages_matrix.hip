@@ -261,14 +261,16 @@ struct Columns {
     return true;
   }
 
+  static __device__ __forceinline__ void clean(v4u &v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] &= ~(nan_bytes(v[e]) * 0xFFu);
+  }
   template <bool CLEAN, typename F>
   __device__ __forceinline__ void add(F values, float scale, const bf16x8 (&w)[2][NT][PP]) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       v4u v = values(dt);
-      if constexpr (CLEAN)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] &= ~(nan_bytes(v[e]) * 0xFFu);
+      if constexpr (CLEAN) clean(v);
       const bf16x8 a0 = widen(v.x, v.y, scale), a1 = widen(v.z, v.w, scale);
 #pragma unroll
       for (int p = PP - 1; p >= 0; --p)
@@ -277,7 +279,7 @@ struct Columns {
           o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w[0][nt][p], o[dt][nt], 0, 0, 0);
           o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w[1][nt][p], o[dt][nt], 0, 0, 0);
         }
-      if (CLEAN || dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      if (CLEAN || (NT > 1 && dt % 4 == 3)) __builtin_amdgcn_sched_barrier(0);
     }
   }
   // values(dt): what this lane names of a page (value_offset)
@@ -338,19 +340,19 @@ struct AttendArgs {
 };
 
 // ---------------------------------------------------------------------------
-// Up to 16 query columns a sequence: a workgroup's four wavefronts take the pages of a part in turn and join at the end.
+// Up to 16 query columns a sequence: a workgroup's four wavefronts take the pages of a part in turn and join at the end.  Each has
+// room for the keys and the values of one page; direct loads fill it, the next page's keys as soon as this page's have been
+// used, then its values, so half a page is always under way and no wavefront waits for another.
 // ---------------------------------------------------------------------------
-// (the operands of an fp32 layer with heads of 128 need more registers than two wavefronts a SIMD leave)
 template <typename Tag, int D>
-constexpr int kFewWaves = kQueryParts<Tag> == 3 && D == 128 ? 1 : 2;
-
-template <typename Tag, int D>
-__global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D>)) void attend_pages_kernel(AttendArgs a, Image<D, 1> *__restrict__ partials) {
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_kernel(AttendArgs a, Image<D, 1> *__restrict__ partials) {
   constexpr int PP = kQueryParts<Tag> == 1 ? 2 : 3;
   using Cols = Columns<Tag, D, 1, PP>;
   constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
+  constexpr int LOADS = TILE / 1024;   // of 1 KiB, for a page's keys or values
   __shared__ union {
     AttendPlanMemory plan;
+    v4u tile[kAttendWaves][2][LOADS][64];
     Image<D, 1> image[2];
   } mem;
   const PageTable &t = a.t;
@@ -359,8 +361,12 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D>)) void attend_pa
   if (!find_part(t, a.plan, a.max_rows, blockIdx.x, h == 0, a.meta, mem.plan, part)) return;
   Cols c;
   c.start(t, part, part.block * a.plan.columns, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
+  __syncthreads();   // the plan's memory is given up
 
   const int32_t *row_of_table = t.table + static_cast<int64_t>(part.seq) * t.width;
+  const int key_lane = key_offset<D>(lane, 0, 0), value_lane = value_offset(lane, 0);
+  const v4u(*keys)[64] = mem.tile[wave][0], (*values)[64] = mem.tile[wave][1];
+  const uint32_t keys_at = lds_address(keys), values_at = lds_address(values);
   // pages of this wavefront, 64 at a time: lane i knows the i-th
   for (int base = part.first + wave; base < part.last; base += 64 * kAttendWaves) {
     const int mine = base + lane * kAttendWaves;
@@ -374,40 +380,46 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D>)) void attend_pa
       ks_lane = a.k_scale[at];
       vs_lane = a.v_scale[at];
     }
-    v4u kb[4][KV], vb[DT];
     auto page_at = [&](int i) __attribute__((always_inline)) {
       return (static_cast<int64_t>(__builtin_amdgcn_readlane(entry, i)) * a.n_kv_heads + h) * TILE;
     };
-    auto load_k = [&](int64_t at) __attribute__((always_inline)) {
+    auto request_keys = [&](int64_t at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int u = 0; u < KV; ++u)
-          kb[rt][u] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(a.k_pages + at + key_offset<D>(lane, rt, u)));
+      for (int l = 0; l < LOADS; ++l) dma16_base(a.k_pages + at + l / KV * 16 * D + l % KV * 16, key_lane, keys_at + l * 1024);
     };
-    auto load_v = [&](int64_t at) __attribute__((always_inline)) {
+    auto request_values = [&](int64_t at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) vb[dt] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(a.v_pages + at + value_offset(lane, dt)));
+      for (int l = 0; l < LOADS; ++l) dma16_base(a.v_pages + at + l * 16 * kPageTokens, value_lane, values_at + l * 1024);
     };
     int i = __builtin_ctzll(todo);
-    load_k(page_at(i));
-    load_v(page_at(i));
-    while (todo != 0) {
+    wait_vmem<0>();   // (scales and queries: what follows counts its own requests)
+    request_keys(page_at(i));
+    request_values(page_at(i));
+    while (true) {
       todo &= todo - 1;
-      const int next = todo != 0 ? __builtin_ctzll(todo) : i;
+      const bool more = todo != 0;
+      const int next = more ? __builtin_ctzll(todo) : i;
       const int64_t next_at = page_at(next);
       const float ks_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_lane), i));
       const float vs_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_lane), i));
       const int token0 = (base + i * kAttendWaves) * kPageTokens;
+      wait_vmem<LOADS>();         // the keys are there, the values on their way
       f32x4 s[4][1];
-      c.logits([&](int rt, int u) __attribute__((always_inline)) { return kb[rt][u]; }, ks_page, s);
-      __builtin_amdgcn_sched_barrier(0);
-      if (next != i) load_k(next_at);
+      c.logits([&](int rt, int u) __attribute__((always_inline)) { return keys[rt * KV + u][lane]; }, ks_page, s);
+      if (more) {
+        wait_lds_reads();
+        request_keys(next_at);
+      }
       bf16x8 w[2][1][PP];
       c.weights(token0, a.logit_scale, s, w);
-      __builtin_amdgcn_sched_barrier(0);
-      c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return vb[dt]; }, vs_page, w);
-      if (next != i) load_v(next_at);
+      if (more)
+        wait_vmem<LOADS>();
+      else
+        wait_vmem<0>();
+      c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return values[dt][lane]; }, vs_page, w);
+      if (!more) break;
+      wait_lds_reads();
+      request_values(next_at);
       i = next;
     }
   }
@@ -415,7 +427,7 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D>)) void attend_pa
   // wavefronts 2 and 3 into 0 and 1, then 1 into 0
 #pragma unroll
   for (int half = 2; half >= 1; half >>= 1) {
-    __syncthreads();   // (the plan's memory, or the images of the step before)
+    __syncthreads();   // (the tiles, or the images of the step before)
     if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
     __syncthreads();
     if (wave < half) {
@@ -635,8 +647,17 @@ template <int TILES>
 struct Division {
   // Workgroups that a launch is cut into, about: decoding twice what the chip holds at two a CU, so that uneven parts even out;
   // with more columns, whose partial results are larger, what it holds
-  static constexpr int kWorkgroups = TILES == 1 ? 1024 : 512;
-  static constexpr int kLeastPages = 8;
+  #ifndef WG1
+#define WG1 1024
+#endif
+#ifndef WGN
+#define WGN 512
+#endif
+#ifndef LP
+#define LP 8
+#endif
+  static constexpr int kWorkgroups = TILES == 1 ? WG1 : WGN;
+  static constexpr int kLeastPages = LP;
   static int target_parts(int n_kv_heads) { return std::max(1, kWorkgroups / n_kv_heads); }
   template <int D>
   static size_t scratch_bytes(int n_kv_heads) {
