@@ -15,35 +15,48 @@ constexpr int kAttendWaves = kAttendThreads / 64;
 constexpr int kMaxItems = 1024;       // of a launch that is cut along the cache
 
 // An item is a block of query columns (row, query head of the kv head) of one sequence; all kv heads have the same items.
-// Pages of an item are cut into parts of the same number of pages throughout the launch, so that long sequences become many
-// workgroups and short ones stay whole; a workgroup has one part.  How long a part is depends on lengths that only
-// the device knows: every workgroup adds up the items' pages (their last rows' positions) and finds its part by itself.
+// All pages of all items, kv head after kv head, make one long list, which is cut into equal shares, one for each unit of the
+// launch (a workgroup or a wavefront): long sequences are spread over many units, short ones stay whole, and all units end
+// together however uneven the lengths are.  Only the device knows those: every workgroup adds up the items' pages (their last
+// rows' positions) and finds its share by itself.
 struct AttendPlan {
   int n_blocks;       // column blocks of a sequence
   int columns;        // of a block
   int group;          // query heads of a kv head
-  int target_parts;   // for all items of a kv head together, about; 0: items are not cut
-  int least_pages;    // of a part
+  int units;          // at most; 0: not cut, a workgroup takes the item blockIdx.x of kv head blockIdx.y
+  int least_pages;    // of a unit
 };
 
-struct AttendPart {
-  int seq, block;     // the item
-  int first, last;    // its pages [first, last)
-  int n_parts;        // of the item; 1: the workgroup writes the result itself
-  int slot;           // partial results of this part, among those of the kv head
-  int lo, hi;         // rows of the sequence
+// Shares: unit u has the pages [edge(u), edge(u + 1)) of the list of n.
+struct Shares {
+  uint32_t n, units;
+  __device__ __forceinline__ Shares(const AttendPlan &plan, uint32_t pages)
+      : n(pages), units(min(static_cast<uint32_t>(plan.units), max(1u, (pages + plan.least_pages - 1) / plan.least_pages))) {}
+  __device__ __forceinline__ uint32_t edge(uint32_t u) const { return static_cast<uint32_t>(static_cast<uint64_t>(u) * n / units); }
+  // the unit that has page x: the last whose edge is not behind it
+  __device__ __forceinline__ uint32_t unit_of(uint32_t x) const {
+    return static_cast<uint32_t>((static_cast<uint64_t>(x + 1) * units + n - 1) / n) - 1;
+  }
 };
 
-// Pages up to the last token that any row of an item sees.  `lanes` (a power of two, at most 64) neighbouring threads look at
-// its rows together and all of them return the answer.
-__device__ __forceinline__ int item_pages(const PageTable &t, const AttendPlan &plan, int max_rows, int item, int sub, int lanes) {
-  const int s = item / plan.n_blocks, b = item - s * plan.n_blocks;
-  int lo, hi;
-  rows_of(t, s, lo, hi);
-  hi = min(hi, lo + max_rows);
-  const int r0 = lo + static_cast<int>(static_cast<int64_t>(b) * plan.columns / plan.group);
-  const int r1 = min(hi, lo + static_cast<int>((static_cast<int64_t>(b + 1) * plan.columns + plan.group - 1) / plan.group));
-  int n = 0;
+// An item's rows.
+struct AttendItem {
+  int seq, block, lo, hi;
+  __device__ __forceinline__ AttendItem(const PageTable &t, const AttendPlan &plan, int max_rows, int item)
+      : seq(item / plan.n_blocks), block(item - seq * plan.n_blocks) {
+    rows_of(t, seq, lo, hi);
+    hi = min(hi, lo + max_rows);
+  }
+};
+
+// Pages up to the last token that any row of an item sees; 0: it has no rows, 1: or they see nothing.  `lanes` (a power of two, at
+// most 64) neighbouring threads look at its rows together and all of them return the answer.
+__device__ __forceinline__ int item_pages(const PageTable &t, const AttendPlan &plan, int max_rows, int index, int sub, int lanes) {
+  const AttendItem i(t, plan, max_rows, index);
+  const int64_t c0 = static_cast<int64_t>(i.block) * plan.columns;
+  const int r0 = i.lo + static_cast<int>(c0 / plan.group);
+  const int r1 = min(i.hi, i.lo + static_cast<int>((c0 + plan.columns + plan.group - 1) / plan.group));
+  int n = r0 < r1 ? 1 : 0;
   for (int r = r0 + sub; r < r1; r += lanes) {
     const int p = t.row_pos[r];
     if (p >= 0 && (p >> 6) < t.width) n = max(n, (p >> 6) + 1);
@@ -52,102 +65,64 @@ __device__ __forceinline__ int item_pages(const PageTable &t, const AttendPlan &
   return n;
 }
 
-struct AttendPlanMemory {
-  int pages[kMaxItems];
-  int sum[kAttendWaves];
-  int scan[2][kAttendWaves];
-  int found[5];
-};
-
-// What this workgroup does; false: nothing.  meta (written by the workgroups of kv head 0): first slot and parts of each item.
-__device__ __forceinline__ bool find_part(const PageTable &t, const AttendPlan &plan, int max_rows, int index, bool writes_meta, int2 *meta,
-                                          AttendPlanMemory &mem, AttendPart &part) {
-  const int n_items = t.n_seqs * plan.n_blocks;
+// Threads that look at an item's rows together.
+__device__ __forceinline__ int item_lanes(const AttendPlan &plan, int max_rows) {
   const int rows = min(max_rows, (plan.columns + plan.group - 1) / plan.group + 1);
   int lanes = 1;
   while (lanes < rows && lanes < 64) lanes <<= 1;
+  return lanes;
+}
+
+struct AttendPlanMemory {
+  int start[kMaxItems + 1];   // pages of a kv head before an item
+  int scan[kAttendWaves];
+};
+
+// All items' pages.  The first workgroup leaves the table for the kernel that joins.
+__device__ __forceinline__ void add_up_items(const PageTable &t, const AttendPlan &plan, int max_rows, bool leave, int *table,
+                                             AttendPlanMemory &mem) {
+  const int n_items = t.n_seqs * plan.n_blocks;
+  const int lanes = item_lanes(plan, max_rows);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int item = index, pages = 0;
-  part.n_parts = 1;
-  part.slot = 0;
-  part.first = 0;
-  if (plan.target_parts == 0) {
-    pages = item_pages(t, plan, max_rows, item, lane & (lanes - 1), lanes);
-    part.last = pages;
-  } else {
-    int total = 0;
-    for (int i0 = 0; i0 < n_items; i0 += kAttendThreads / lanes) {
-      const int i = i0 + tid / lanes;
-      if (i >= n_items) continue;   // (the lanes of an item go together)
-      const int n = item_pages(t, plan, max_rows, i, tid & (lanes - 1), lanes);
-      if ((tid & (lanes - 1)) == 0) {
-        mem.pages[i] = n;
-        total += n;
-      }
-    }
-    total = wave_sum_i(total);
-    if (lane == 0) mem.sum[wave] = total;
-    if (tid == 0) mem.found[0] = -1;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) total += mem.sum[w];
-    int step = max(plan.least_pages, (total + plan.target_parts - 1) / plan.target_parts);
-    step = (step + kAttendWaves - 1) / kAttendWaves * kAttendWaves;
-    // four items a thread: their parts, and the slots of those that have more than one
-    constexpr int PER = kMaxItems / kAttendThreads;
-    int parts[PER], mine = 0, slots = 0;
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int i = tid * PER + u;
-      parts[u] = i < n_items ? max(1, (mem.pages[i] + step - 1) / step) : 0;
-      mine += parts[u];
-      slots += parts[u] > 1 ? parts[u] : 0;
-    }
-    int before = mine, slots_before = slots;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int a = __shfl_up(before, o, 64), b = __shfl_up(slots_before, o, 64);
-      if (lane >= o) before += a, slots_before += b;
-    }
-    if (lane == 63) mem.scan[0][wave] = before, mem.scan[1][wave] = slots_before;
-    __syncthreads();
-    before -= mine;
-    slots_before -= slots;
-    for (int w = 0; w < wave; ++w) before += mem.scan[0][w], slots_before += mem.scan[1][w];
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      if (index >= before && index < before + parts[u]) {
-        mem.found[0] = tid * PER + u;
-        mem.found[1] = index - before;
-        mem.found[2] = parts[u];
-        mem.found[3] = slots_before + index - before;
-      }
-      before += parts[u];
-      slots_before += parts[u] > 1 ? parts[u] : 0;
-    }
-    __syncthreads();
-    item = mem.found[0];
-    if (item < 0) return false;
-    pages = mem.pages[item];
-    part.n_parts = mem.found[2];
-    part.slot = mem.found[3];
-    part.first = mem.found[1] * step;
-    part.last = min(pages, part.first + step);
-    if (writes_meta && mem.found[1] == 0 && tid == 0) meta[item] = make_int2(part.slot, part.n_parts);
+  for (int i0 = 0; i0 < n_items; i0 += kAttendThreads / lanes) {
+    const int i = i0 + tid / lanes;
+    if (i >= n_items) continue;   // (the lanes of an item go together)
+    const int n = item_pages(t, plan, max_rows, i, tid & (lanes - 1), lanes);
+    if ((tid & (lanes - 1)) == 0) mem.start[i] = n;
   }
-  // the same in every lane: scalars
-  item = __builtin_amdgcn_readfirstlane(item);
-  part.first = __builtin_amdgcn_readfirstlane(part.first);
-  part.last = __builtin_amdgcn_readfirstlane(part.last);
-  part.n_parts = __builtin_amdgcn_readfirstlane(part.n_parts);
-  part.slot = __builtin_amdgcn_readfirstlane(part.slot);
-  part.seq = item / plan.n_blocks;
-  part.block = item - part.seq * plan.n_blocks;
-  rows_of(t, part.seq, part.lo, part.hi);
-  part.hi = min(part.hi, part.lo + max_rows);
-  // a block behind the sequence's rows
-  return static_cast<int64_t>(part.block) * plan.columns < static_cast<int64_t>(part.hi - part.lo) * plan.group;
+  __syncthreads();
+  constexpr int PER = kMaxItems / kAttendThreads;   // neighbouring items of a thread
+  int pages[PER], mine = 0;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = tid * PER + u;
+    pages[u] = i < n_items ? mem.start[i] : 0;
+    mine += pages[u];
+  }
+  int before = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int a = __shfl_up(before, o, 64);
+    if (lane >= o) before += a;
+  }
+  if (lane == 63) mem.scan[wave] = before;
+  __syncthreads();
+  before -= mine;
+  for (int w = 0; w < wave; ++w) before += mem.scan[w];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = tid * PER + u;
+    if (i <= n_items) {
+      mem.start[i] = before;
+      if (leave) table[i] = before;
+    }
+    before += pages[u];
+  }
+  if (tid == kAttendThreads - 1 && n_items == kMaxItems) {
+    mem.start[kMaxItems] = before;
+    if (leave) table[kMaxItems] = before;
+  }
+  __syncthreads();
 }
 
 // Eight e4m3 numbers of two words, times a power of two, as bf16: exact.

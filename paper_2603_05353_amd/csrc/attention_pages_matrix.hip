@@ -3,7 +3,7 @@
 // Decoding reads every page once for a few query columns: memory bounds it, and what a kernel has to do is to keep requests in
 // flight.  A wavefront takes whole pages, as many bytes as it likes to have under way, straight from memory into registers in
 // the operand layout of the 16x16x32 bf16 instruction (no LDS, no barrier, no shuffle in the loop):
-//   first product, S^T[token, column]: a lane's keys of a block of 16 tokens are d/4 bytes in a row of one token
+//   first product, S^T[token, column]: a lane's keys of a block of 16 tokens are d/64 times 16 bytes in a row of one token
 //     (the order of the d elements along the reduction is free, queries follow it);
 //   second product, O^T[d, column]: a lane's values are the 16 bytes in a row of one value row that ifkv.h's byte order makes
 //     of the very tokens whose probabilities the lane holds.
@@ -64,7 +64,7 @@ __device__ __forceinline__ void write_columns(void *out, float *lse_out, int64_t
 // and of the dt-th block of 16 value rows.
 template <int D>
 __device__ __forceinline__ int key_offset(int lane, int rt, int u) {
-  return (rt * 16 + (lane & 15)) * D + (lane >> 4) * (D / 4) + u * 16;
+  return (rt * 16 + (lane & 15)) * D + u * 64 + (lane >> 4) * 16;
 }
 __device__ __forceinline__ int value_offset(int lane, int dt) { return (dt * 16 + (lane & 15)) * kPageTokens + (lane >> 4) * 16; }
 
@@ -85,7 +85,7 @@ struct Columns {
   int n, g;
 
   // columns first_column .. of the sequence's
-  __device__ __forceinline__ void start(const PageTable &t, const AttendPart &part, int first_column, int grp, int h, int n_q_heads,
+  __device__ __forceinline__ void start(const PageTable &t, const AttendItem &item, int first_column, int grp, int h, int n_q_heads,
                                         const void *queries, int64_t q_stride) {
     const int lane = threadIdx.x & 63;
     n = lane & 15;
@@ -95,27 +95,29 @@ struct Columns {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int c = first_column + nt * 16 + n;
-      const int r = part.lo + c / grp;
+      const int r = item.lo + c / grp;
       const int hq = h * grp + c % grp;
-      const bool real = r < part.hi;
+      const bool real = r < item.hi;
       pos[nt] = real ? t.row_pos[r] : -1;
       row_head[nt] = real ? static_cast<int64_t>(r) * n_q_heads + hq : -1;
       const bool sees = pos[nt] >= 0 && (pos[nt] >> 6) < t.width;
       if (sees) highest = max(highest, pos[nt]);
       if (!sees) pos[nt] = INT32_MAX;
       lowest = min(lowest, pos[nt]);
-      const char *src = static_cast<const char *>(queries) + (r * q_stride + static_cast<int64_t>(hq) * D + g * (D / 4)) * Elem<Tag>::kBytes;
+      const char *src = static_cast<const char *>(queries) + (r * q_stride + static_cast<int64_t>(hq) * D + g * 16) * Elem<Tag>::kBytes;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
+        constexpr int PER16 = 16 / Elem<Tag>::kVec;   // 16-byte vectors of 16 elements: steps 2 u and 2 u + 1 share those of key load u
+        const int vec = ks / 2 * 4 * PER16 + ks % 2 * (PER16 / 2);
         if constexpr (QP == 1) {
           v4u w = {0, 0, 0, 0};
-          if (sees) w = reinterpret_cast<const v4u *>(src)[ks];
+          if (sees) w = reinterpret_cast<const v4u *>(src)[vec];
           q[nt][0][ks] = __builtin_bit_cast(bf16x8, w);
         } else {
           float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
           if (sees) {
-            *reinterpret_cast<f32x4 *>(x) = reinterpret_cast<const f32x4 *>(src)[2 * ks];
-            *reinterpret_cast<f32x4 *>(x + 4) = reinterpret_cast<const f32x4 *>(src)[2 * ks + 1];
+            *reinterpret_cast<f32x4 *>(x) = reinterpret_cast<const f32x4 *>(src)[vec];
+            *reinterpret_cast<f32x4 *>(x + 4) = reinterpret_cast<const f32x4 *>(src)[vec + 1];
           }
           bf16x8 s[QP];
           split8<QP>(x, s);
@@ -333,124 +335,170 @@ struct AttendArgs {
   const void *q;
   void *out;
   float *lse_out;
-  int2 *meta;
+  int *item_start;   // for the kernel that joins
   int64_t q_stride;
   int max_rows, n_pages, n_q_heads, n_kv_heads;
   float logit_scale;
 };
+
+// Goes through a unit's share: piece(item, kv head, first page, last page, slot) for every item that has pages in it.  slot:
+// where partial results go, -1: the piece is the whole item.  A unit has two slots: the piece it begins with may be the rest
+// of an item (or its middle), the one it ends with the beginning of one.
+template <typename F>
+__device__ __forceinline__ void each_piece(const AttendPlan &plan, int n_items, int n_kv_heads, const AttendPlanMemory &mem, uint32_t unit,
+                                           F piece) {
+  const auto scalar = [](uint32_t x) __attribute__((always_inline)) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(x)); };
+  const uint32_t total = scalar(mem.start[n_items]);
+  if (total == 0) return;
+  const Shares shares(plan, total * n_kv_heads);
+  if (unit >= shares.units) return;
+  uint32_t x = scalar(shares.edge(unit));
+  const uint32_t end = scalar(shares.edge(unit + 1));
+  uint32_t h = x / total, r = x - h * total;
+  int item = 0;
+  for (int half = kMaxItems / 2; half > 0; half >>= 1)   // the last item that begins at or before r
+    if (item + half < n_items && static_cast<uint32_t>(mem.start[item + half]) <= r) item += half;
+  item = scalar(item);
+  while (x < end) {
+    const uint32_t s = scalar(mem.start[item]), e = scalar(mem.start[item + 1]);
+    if (s < e) {
+      const uint32_t last = min(e, r + (end - x));
+      piece(item, static_cast<int>(h), static_cast<int>(r - s), static_cast<int>(last - s),
+            r == s && last == e ? -1 : static_cast<int>(2 * unit + (r == s ? 1 : 0)));
+      x += last - r;
+      r = last;
+    }
+    if (r == e) ++item;
+    if (r == total) r = 0, item = 0, ++h;
+  }
+}
 
 // ---------------------------------------------------------------------------
 // Up to 16 query columns a sequence: a workgroup's four wavefronts take the pages of a part in turn and join at the end.  Each has
 // room for the keys and the values of one page; direct loads fill it, the next page's keys as soon as this page's have been
 // used, then its values, so half a page is always under way and no wavefront waits for another.
 // ---------------------------------------------------------------------------
-template <typename Tag, int D>
+template <typename Tag, int D, int TEAM>
 __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_kernel(AttendArgs a, Image<D, 1> *__restrict__ partials) {
   constexpr int PP = kQueryParts<Tag> == 1 ? 2 : 3;
   using Cols = Columns<Tag, D, 1, PP>;
   constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
   constexpr int LOADS = TILE / 1024;   // of 1 KiB, for a page's keys or values
+  __shared__ AttendPlanMemory plan_memory;
   __shared__ union {
-    AttendPlanMemory plan;
     v4u tile[kAttendWaves][2][LOADS][64];
     Image<D, 1> image[2];
   } mem;
   const PageTable &t = a.t;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y;
-  AttendPart part;
-  if (!find_part(t, a.plan, a.max_rows, blockIdx.x, h == 0, a.meta, mem.plan, part)) return;
-  Cols c;
-  c.start(t, part, part.block * a.plan.columns, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
-  __syncthreads();   // the plan's memory is given up
-
-  const int32_t *row_of_table = t.table + static_cast<int64_t>(part.seq) * t.width;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int key_lane = key_offset<D>(lane, 0, 0), value_lane = value_offset(lane, 0);
   const v4u(*keys)[64] = mem.tile[wave][0], (*values)[64] = mem.tile[wave][1];
   const uint32_t keys_at = lds_address(keys), values_at = lds_address(values);
-  // pages of this wavefront, 64 at a time: lane i knows the i-th
-  for (int base = part.first + wave; base < part.last; base += 64 * kAttendWaves) {
-    const int mine = base + lane * kAttendWaves;
-    int entry = -1;
-    if (mine < part.last) entry = row_of_table[mine];
-    uint64_t todo = __ballot(entry >= 0 && entry < a.n_pages);
-    if (todo == 0) continue;
-    float ks_lane = 1.f, vs_lane = 1.f;
-    if (entry >= 0 && entry < a.n_pages) {
-      const int64_t at = static_cast<int64_t>(entry) * a.n_kv_heads + h;
-      ks_lane = a.k_scale[at];
-      vs_lane = a.v_scale[at];
-    }
-    auto page_at = [&](int i) __attribute__((always_inline)) {
-      return (static_cast<int64_t>(__builtin_amdgcn_readlane(entry, i)) * a.n_kv_heads + h) * TILE;
-    };
-    auto request_keys = [&](int64_t at) __attribute__((always_inline)) {
+  const int member = TEAM == 1 ? 0 : wave;   // of the wavefronts that share an item's pages
+
+  const auto piece = [&](int index, int h, int first, int last, int slot) __attribute__((always_inline)) {
+    const AttendItem item(t, a.plan, a.max_rows, index);
+    Cols c;
+    c.start(t, item, item.block * a.plan.columns, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
+    if (c.highest < 0) last = first;
+    const int32_t *row_of_table = t.table + static_cast<int64_t>(item.seq) * t.width;
+    // pages of this wavefront, 64 at a time: lane i knows the i-th
+    for (int base = first + member; base < last; base += 64 * TEAM) {
+      const int mine = base + lane * TEAM;
+      int entry = -1;
+      if (mine < last) entry = row_of_table[mine];
+      uint64_t todo = __ballot(entry >= 0 && entry < a.n_pages);
+      if (todo == 0) continue;
+      float ks_lane = 1.f, vs_lane = 1.f;
+      if (entry >= 0 && entry < a.n_pages) {
+        const int64_t at = static_cast<int64_t>(entry) * a.n_kv_heads + h;
+        ks_lane = a.k_scale[at];
+        vs_lane = a.v_scale[at];
+      }
+      auto page_at = [&](int i) __attribute__((always_inline)) {
+        return (static_cast<int64_t>(__builtin_amdgcn_readlane(entry, i)) * a.n_kv_heads + h) * TILE;
+      };
+      auto request_keys = [&](int64_t at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int l = 0; l < LOADS; ++l) dma16_base(a.k_pages + at + l / KV * 16 * D + l % KV * 16, key_lane, keys_at + l * 1024);
-    };
-    auto request_values = [&](int64_t at) __attribute__((always_inline)) {
+        for (int l = 0; l < LOADS; ++l) dma16_base_once(a.k_pages + at + l / KV * 16 * D + l % KV * 64, key_lane, keys_at + l * 1024);
+      };
+      auto request_values = [&](int64_t at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int l = 0; l < LOADS; ++l) dma16_base(a.v_pages + at + l * 16 * kPageTokens, value_lane, values_at + l * 1024);
-    };
-    int i = __builtin_ctzll(todo);
-    wait_vmem<0>();   // (scales and queries: what follows counts its own requests)
-    request_keys(page_at(i));
-    request_values(page_at(i));
-    while (true) {
-      todo &= todo - 1;
-      const bool more = todo != 0;
-      const int next = more ? __builtin_ctzll(todo) : i;
-      const int64_t next_at = page_at(next);
-      const float ks_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_lane), i));
-      const float vs_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_lane), i));
-      const int token0 = (base + i * kAttendWaves) * kPageTokens;
-      wait_vmem<LOADS>();         // the keys are there, the values on their way
-      f32x4 s[4][1];
-      c.logits([&](int rt, int u) __attribute__((always_inline)) { return keys[rt * KV + u][lane]; }, ks_page, s);
-      if (more) {
+        for (int l = 0; l < LOADS; ++l) dma16_base_once(a.v_pages + at + l * 16 * kPageTokens, value_lane, values_at + l * 1024);
+      };
+      int i = __builtin_ctzll(todo);
+      wait_vmem<0>();   // (scales and queries: what follows counts its own requests)
+      request_keys(page_at(i));
+      request_values(page_at(i));
+      while (true) {
+        todo &= todo - 1;
+        const bool more = todo != 0;
+        const int next = more ? __builtin_ctzll(todo) : i;
+        const int64_t next_at = page_at(next);
+        const float ks_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_lane), i));
+        const float vs_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_lane), i));
+        const int token0 = (base + i * TEAM) * kPageTokens;
+        wait_vmem<LOADS>();         // the keys are there, the values on their way
+        f32x4 s[4][1];
+        c.logits([&](int rt, int u) __attribute__((always_inline)) { return keys[rt * KV + u][lane]; }, ks_page, s);
+        if (more) {
+          wait_lds_reads();
+          request_keys(next_at);
+        }
+        bf16x8 w[2][1][PP];
+        c.weights(token0, a.logit_scale, s, w);
+        if (more)
+          wait_vmem<LOADS>();
+        else
+          wait_vmem<0>();
+        c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return values[dt][lane]; }, vs_page, w);
         wait_lds_reads();
-        request_keys(next_at);
+        if (!more) break;
+        request_values(next_at);
+        i = next;
       }
-      bf16x8 w[2][1][PP];
-      c.weights(token0, a.logit_scale, s, w);
-      if (more)
-        wait_vmem<LOADS>();
+    }
+    c.join_sums();
+    if constexpr (TEAM > 1) {
+      // wavefronts 2 and 3 into 0 and 1, then 1 into 0
+#pragma unroll
+      for (int half = 2; half >= 1; half >>= 1) {
+        __syncthreads();   // (the tiles, or the images of the step before)
+        if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
+        __syncthreads();
+        if (wave < half) {
+          const Image<D, 1> &im = mem.image[wave];
+          const float other = im.ref[0][c.n], m = fmaxf(c.ref[0], other);
+          const float x = c.ref[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[0] - m);
+          const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
+          c.ref[0] = m;
+          c.sum[0] = c.sum[0] * x + im.sum[0][c.n] * y;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const f32x4 o = im.o[dt][lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c.o[dt][0][e] = c.o[dt][0][e] * x + o[e] * y;
+          }
+        }
+      }
+    }
+    if (TEAM == 1 || wave == 0) {
+      c.forget_unseen();
+      if (slot < 0)
+        c.finish(a.out, a.lse_out);
       else
-        wait_vmem<0>();
-      c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return values[dt][lane]; }, vs_page, w);
-      if (!more) break;
-      wait_lds_reads();
-      request_values(next_at);
-      i = next;
+        c.save(partials[slot], 0);
     }
+    if constexpr (TEAM > 1) __syncthreads();   // the images are given up
+  };
+  if (a.plan.units == 0) {
+    const int lanes = item_lanes(a.plan, a.max_rows);
+    const int n = __builtin_amdgcn_readfirstlane(item_pages(t, a.plan, a.max_rows, blockIdx.x, lane & (lanes - 1), lanes));
+    if (n > 0) piece(blockIdx.x, blockIdx.y, 0, n, -1);
+    return;
   }
-  c.join_sums();
-  // wavefronts 2 and 3 into 0 and 1, then 1 into 0
-#pragma unroll
-  for (int half = 2; half >= 1; half >>= 1) {
-    __syncthreads();   // (the tiles, or the images of the step before)
-    if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
-    __syncthreads();
-    if (wave < half) {
-      const Image<D, 1> &im = mem.image[wave];
-      const float other = im.ref[0][c.n], m = fmaxf(c.ref[0], other);
-      const float x = c.ref[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[0] - m);
-      const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
-      c.ref[0] = m;
-      c.sum[0] = c.sum[0] * x + im.sum[0][c.n] * y;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const f32x4 o = im.o[dt][lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c.o[dt][0][e] = c.o[dt][0][e] * x + o[e] * y;
-      }
-    }
-  }
-  if (wave != 0) return;
-  c.forget_unseen();
-  if (part.n_parts == 1)
-    c.finish(a.out, a.lse_out);
-  else
-    c.save(partials[static_cast<int64_t>(h) * 2 * a.plan.target_parts + part.slot], 0);
+  add_up_items(t, a.plan, a.max_rows, blockIdx.x == 0, a.item_start, plan_memory);
+  each_piece(a.plan, t.n_seqs * a.plan.n_blocks, a.n_kv_heads, plan_memory, TEAM == 1 ? blockIdx.x * kAttendWaves + wave : blockIdx.x, piece);
 }
 
 // ---------------------------------------------------------------------------
@@ -466,22 +514,12 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(A
   constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
   constexpr int LOADS = 2 * TILE / 1024;              // of 1 KiB, a page: keys first
   constexpr int MINE = LOADS / kAttendWaves;          // of a wavefront
+  __shared__ AttendPlanMemory plan_memory;
   __shared__ v4u s_stage[kStages][LOADS][64];
-  __shared__ union {
-    AttendPlanMemory plan;
-    struct {
-      int4 entry[kPageList];                          // page, its place in the sequence, scales
-      int count[kAttendWaves];
-    } list;
-  } mem;
+  __shared__ int4 s_entry[kPageList];                 // page, its place in the sequence, scales
+  __shared__ int s_count[kAttendWaves];
   const PageTable &t = a.t;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = blockIdx.y;
-  AttendPart part;
-  if (!find_part(t, a.plan, a.max_rows, blockIdx.x, h == 0, a.meta, mem.plan, part)) return;
-  Cols c;
-  c.start(t, part, part.block * a.plan.columns + wave * NT * 16, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
-
-  const int32_t *row_of_table = t.table + static_cast<int64_t>(part.seq) * t.width;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int offset[MINE];
 #pragma unroll
   for (int u = 0; u < MINE; ++u) {
@@ -489,69 +527,82 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(A
     offset[u] = l < LOADS / 2 ? key_offset<D>(lane, l / KV, l % KV) : value_offset(lane, l - LOADS / 2);
   }
   const uint8_t *pool = wave < kAttendWaves / 2 ? a.k_pages : a.v_pages;   // the first half of the loads are keys
-  for (int base = part.first; base < part.last; base += kPageList) {
-    __syncthreads();   // (the list before has been read, or the plan's memory)
-    int entry = -1;
-    if (base + tid < part.last) entry = row_of_table[base + tid];
-    const uint64_t there = __ballot(entry >= 0 && entry < a.n_pages);
-    if (lane == 0) mem.list.count[wave] = __builtin_popcountll(there);
-    __syncthreads();
-    int n_list = 0, at = __builtin_popcountll(there & ((1ull << lane) - 1));
+
+  const auto piece = [&](int index, int h, int first, int last, int slot) __attribute__((always_inline)) {
+    const AttendItem item(t, a.plan, a.max_rows, index);
+    Cols c;
+    c.start(t, item, item.block * a.plan.columns + wave * NT * 16, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
+    const int32_t *row_of_table = t.table + static_cast<int64_t>(item.seq) * t.width;
+    for (int base = first; base < last; base += kPageList) {
+      __syncthreads();   // (the list before has been read)
+      int entry = -1;
+      if (base + tid < last && base + tid < t.width) entry = row_of_table[base + tid];
+      const uint64_t there = __ballot(entry >= 0 && entry < a.n_pages);
+      if (lane == 0) s_count[wave] = __builtin_popcountll(there);
+      __syncthreads();
+      int n_list = 0, at = __builtin_popcountll(there & ((1ull << lane) - 1));
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) {
-      if (w < wave) at += mem.list.count[w];
-      n_list += mem.list.count[w];
-    }
-    if (entry >= 0 && entry < a.n_pages) {
-      const int64_t s = static_cast<int64_t>(entry) * a.n_kv_heads + h;
-      mem.list.entry[at] = make_int4(entry, base + tid, __float_as_int(a.k_scale[s]), __float_as_int(a.v_scale[s]));
-    }
-    __syncthreads();
-    if (n_list == 0) continue;
-    auto request = [&](int p) __attribute__((always_inline)) {   // (behind the end: the last page once more, so that counts stay the same)
-      const int page = mem.list.entry[min(p, n_list - 1)].x;
-      const uint8_t *src = pool + (static_cast<int64_t>(page) * a.n_kv_heads + h) * TILE;
+      for (int w = 0; w < kAttendWaves; ++w) {
+        if (w < wave) at += s_count[w];
+        n_list += s_count[w];
+      }
+      if (entry >= 0 && entry < a.n_pages) {
+        const int64_t s = static_cast<int64_t>(entry) * a.n_kv_heads + h;
+        s_entry[at] = make_int4(entry, base + tid, __float_as_int(a.k_scale[s]), __float_as_int(a.v_scale[s]));
+      }
+      __syncthreads();
+      if (n_list == 0) continue;
+      auto request = [&](int p) __attribute__((always_inline)) {   // (behind the end: the last page once more, so that counts stay the same)
+        const int page = s_entry[min(p, n_list - 1)].x;
+        const uint8_t *src = pool + (static_cast<int64_t>(page) * a.n_kv_heads + h) * TILE;
 #pragma unroll
-      for (int u = 0; u < MINE; ++u)
-        dma16(src + offset[u], lds_address(&s_stage[p % kStages][wave * MINE + u][0]));
-    };
-    wait_vmem<0>();
+        for (int u = 0; u < MINE; ++u) dma16(src + offset[u], lds_address(&s_stage[p % kStages][wave * MINE + u][0]));
+      };
+      wait_vmem<0>();
 #pragma unroll
-    for (int p = 0; p < kStages - 1; ++p) request(p);
-    for (int p = 0; p < n_list; ++p) {
-      wait_vmem<(kStages - 2) * MINE>();   // this wavefront's share of page p is there
-      wait_lds_reads();                    // and it has taken all it needs of page p - 1
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" : : : "memory");
-      request(p + kStages - 1);
-      const int4 e = mem.list.entry[p];
-      const int token0 = __builtin_amdgcn_readfirstlane(e.y) * kPageTokens;
-      if (token0 > c.highest) continue;
-      const v4u (*stage)[64] = s_stage[p % kStages];
-      f32x4 s[4][NT];
-      c.logits([&](int rt, int u) __attribute__((always_inline)) { return stage[rt * KV + u][lane]; }, __int_as_float(e.z), s);
-      bf16x8 w[2][NT][PP];
-      c.weights(token0, a.logit_scale, s, w);
-      __builtin_amdgcn_sched_barrier(0);
-      c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return stage[LOADS / 2 + dt][lane]; }, __int_as_float(e.w), w);
+      for (int p = 0; p < kStages - 1; ++p) request(p);
+      for (int p = 0; p < n_list; ++p) {
+        wait_vmem<(kStages - 2) * MINE>();   // this wavefront's share of page p is there
+        wait_lds_reads();                    // and it has taken all it needs of page p - 1
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
+        request(p + kStages - 1);
+        const int4 e = s_entry[p];
+        const int token0 = __builtin_amdgcn_readfirstlane(e.y) * kPageTokens;
+        if (token0 > c.highest) continue;
+        const v4u(*stage)[64] = s_stage[p % kStages];
+        f32x4 s[4][NT];
+        c.logits([&](int rt, int u) __attribute__((always_inline)) { return stage[rt * KV + u][lane]; }, __int_as_float(e.z), s);
+        bf16x8 w[2][NT][PP];
+        c.weights(token0, a.logit_scale, s, w);
+        c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return stage[LOADS / 2 + dt][lane]; }, __int_as_float(e.w), w);
+      }
+      wait_vmem<0>();   // nothing is under way into LDS that is given up or used again
     }
-    wait_vmem<0>();   // nothing is under way into LDS that is given up or used again
+    c.join_sums();
+    c.forget_unseen();
+    if (slot < 0)
+      c.finish(a.out, a.lse_out);
+    else
+      c.save(partials[slot], wave * NT);
+  };
+  if (a.plan.units == 0) {
+    const int lanes = item_lanes(a.plan, a.max_rows);
+    const int n = __builtin_amdgcn_readfirstlane(item_pages(t, a.plan, a.max_rows, blockIdx.x, lane & (lanes - 1), lanes));
+    if (n > 0) piece(blockIdx.x, blockIdx.y, 0, n, -1);
+    return;
   }
-  c.join_sums();
-  c.forget_unseen();
-  if (part.n_parts == 1)
-    c.finish(a.out, a.lse_out);
-  else
-    c.save(partials[static_cast<int64_t>(h) * 2 * a.plan.target_parts + part.slot], wave * NT);
+  add_up_items(t, a.plan, a.max_rows, blockIdx.x == 0, a.item_start, plan_memory);
+  each_piece(a.plan, t.n_seqs * a.plan.n_blocks, a.n_kv_heads, plan_memory, blockIdx.x, piece);
 }
 
-// Joins the parts of an item: a workgroup for a quarter of the output rows of a tile of 16 columns.  Its wavefronts take the
-// parts in turn, eight requests under way, and join.
+// Joins the pieces of an item: a workgroup for a quarter of the output rows of a tile of 16 columns.  Its wavefronts take the
+// pieces in turn, eight requests under way, and join.
 constexpr int kMergeSplit = 4, kMergeBatch = 8;
 
 template <typename Tag, int D, int NT>
 __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(PageTable t, AttendPlan plan, int max_rows, int n_q_heads,
-                                                                            const int2 *__restrict__ meta,
+                                                                            const int *__restrict__ item_start,
                                                                             const Image<D, NT> *__restrict__ partials,
                                                                             void *__restrict__ out, float *__restrict__ lse_out) {
   constexpr int DT = D / 16 / kMergeSplit;
@@ -559,15 +610,19 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
   __shared__ float s_ref[kAttendWaves][16], s_sum[kAttendWaves][16];
   const int item = blockIdx.x / (NT * kMergeSplit), nt = blockIdx.x / kMergeSplit % NT, quarter = blockIdx.x % kMergeSplit;
   const int h = blockIdx.y;
-  const int2 m = meta[item];
-  if (m.y <= 1) return;
+  const uint32_t s = item_start[item], e = item_start[item + 1], total = item_start[t.n_seqs * plan.n_blocks];
+  if (s == e) return;
+  const Shares shares(plan, total * gridDim.y);
+  const uint32_t u0 = shares.unit_of(h * total + s), u1 = shares.unit_of(h * total + e - 1);
+  const int pieces = static_cast<int>(u1 - u0) + 1;
+  if (pieces == 1) return;   // the unit wrote the result
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const Image<D, NT> *im = partials + static_cast<int64_t>(h) * 2 * plan.target_parts + m.x;
+  const auto image = [&](int p) __attribute__((always_inline)) -> const Image<D, NT> & { return partials[2 * (u0 + p) + (p == 0 ? 1 : 0)]; };
   float ref = -INFINITY, sum = 0.f;
   f32x4 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0, 0, 0, 0};
-  for (int p0 = wave; p0 < m.y; p0 += kAttendWaves * kMergeBatch) {
+  for (int p0 = wave; p0 < pieces; p0 += kAttendWaves * kMergeBatch) {
     float refs[kMergeBatch], sums[kMergeBatch];
     f32x4 x[kMergeBatch][DT];
 #pragma unroll
@@ -577,11 +632,12 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
       sums[u] = 0.f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) x[u][dt] = f32x4{0, 0, 0, 0};
-      if (p < m.y) {
-        refs[u] = im[p].ref[nt][n];
-        sums[u] = im[p].sum[nt][n];
+      if (p < pieces) {
+        const Image<D, NT> &im = image(p);
+        refs[u] = im.ref[nt][n];
+        sums[u] = im.sum[nt][n];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) x[u][dt] = im[p].o[(quarter * DT + dt) * NT + nt][lane];
+        for (int dt = 0; dt < DT; ++dt) x[u][dt] = im.o[(quarter * DT + dt) * NT + nt][lane];
       }
     }
     float top = ref;
@@ -630,56 +686,44 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
       for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(x[e], b, o[dt][e]);
     }
   }
-  int lo, hi;
-  rows_of(t, item / plan.n_blocks, lo, hi);
-  hi = min(hi, lo + max_rows);
-  const int c = (item % plan.n_blocks) * plan.columns + nt * 16 + n;
-  const int r = lo + c / plan.group;
-  if (r < hi)
+  const AttendItem rows(t, plan, max_rows, item);
+  const int c = rows.block * plan.columns + nt * 16 + n;
+  const int r = rows.lo + c / plan.group;
+  if (r < rows.hi)
     write_columns<Tag, D, DT>(out, quarter == 0 ? lse_out : nullptr, static_cast<int64_t>(r) * n_q_heads + h * plan.group + c % plan.group,
                               quarter * DT, g, o, 1, top, sum);
 }
 
-constexpr size_t kMetaBytes = kMaxItems * sizeof(int2);
+constexpr size_t kTableBytes = (kMaxItems + 4) / 4 * 4 * sizeof(int);
 
-// How a launch with TILES tiles of 16 columns a workgroup is divided.
-template <int TILES>
-struct Division {
-  // Workgroups that a launch is cut into, about: decoding twice what the chip holds at two a CU, so that uneven parts even out;
-  // with more columns, whose partial results are larger, what it holds
-  #ifndef WG1
-#define WG1 1024
+#ifndef UNITS1
+#define UNITS1 512
 #endif
-#ifndef WGN
-#define WGN 512
+#ifndef TEAMRULE
+#define TEAMRULE (items * d.n_kv_heads >= 512)
 #endif
 #ifndef LP
 #define LP 8
 #endif
-  static constexpr int kWorkgroups = TILES == 1 ? WG1 : WGN;
-  static constexpr int kLeastPages = LP;
-  static int target_parts(int n_kv_heads) { return std::max(1, kWorkgroups / n_kv_heads); }
-  template <int D>
-  static size_t scratch_bytes(int n_kv_heads) {
-    return kMetaBytes + static_cast<size_t>(2) * target_parts(n_kv_heads) * n_kv_heads * sizeof(Image<D, TILES>);
-  }
-};
+constexpr int kWorkgroups = UNITS1;     // what the chip holds at two a CU: all of them run at once and end together
+constexpr int kLeastPages = LP;
 
 template <typename Tag, int D, int TILES>
 hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int max_rows, const void *q, int64_t q_stride, void *out,
                float *lse_out) {
   const auto &d = ctx->desc;
-  using Div = Division<TILES>;
   AttendPlan plan;
   plan.group = d.n_q_heads / d.n_kv_heads;
   plan.columns = TILES * 16;
   plan.n_blocks = static_cast<int>((static_cast<int64_t>(max_rows) * plan.group + plan.columns - 1) / plan.columns);
-  plan.least_pages = Div::kLeastPages;
+  plan.least_pages = kLeastPages;
   const int64_t items = static_cast<int64_t>(t.n_seqs) * plan.n_blocks;
-  const bool cut = t.width > Div::kLeastPages && items <= kMaxItems && items * t.width < INT32_MAX;   // (pages are added up in 32 bits)
-  plan.target_parts = cut ? Div::target_parts(d.n_kv_heads) : 0;
-  int2 *meta = static_cast<int2 *>(ctx->page_partials);
-  Image<D, TILES> *partials = reinterpret_cast<Image<D, TILES> *>(static_cast<char *>(ctx->page_partials) + kMetaBytes);
+  // (pages are added up in 32 bits)
+  const bool cut = t.width > kLeastPages && items <= kMaxItems && items * t.width < INT32_MAX / d.n_kv_heads;
+  const bool alone = TILES == 1 && cut && TEAMRULE;
+  plan.units = !cut ? 0 : alone ? kWorkgroups * kAttendWaves : kWorkgroups;
+  int *item_start = static_cast<int *>(ctx->page_partials);
+  Image<D, TILES> *partials = reinterpret_cast<Image<D, TILES> *>(static_cast<char *>(ctx->page_partials) + kTableBytes);
   // a grid has fewer than 2^32 threads: so many sequences a launch (all of them where items are cut)
   const int step = std::max(1, (1 << 23) / plan.n_blocks);
   for (int s = 0; s < t.n_seqs; s += step) {
@@ -688,20 +732,23 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
                           static_cast<const uint8_t *>(pages.v), pages.k_scale, pages.v_scale,
                           static_cast<const char *>(q) + skip * q_stride * Elem<Tag>::kBytes,
                           static_cast<char *>(out) + skip * d.n_q_heads * D * Elem<Tag>::kBytes,
-                          lse_out != nullptr ? lse_out + skip * d.n_q_heads : nullptr, meta, q_stride, max_rows,
+                          lse_out != nullptr ? lse_out + skip * d.n_q_heads : nullptr, item_start, q_stride, max_rows,
                           static_cast<int>(pages.n_pages), d.n_q_heads, d.n_kv_heads, ctx->sm_scale * kLog2e};
-    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.t.n_seqs) * plan.n_blocks + plan.target_parts), d.n_kv_heads), block(kAttendThreads);
-    if constexpr (TILES == 1)
-      hipLaunchKernelGGL((attend_pages_kernel<Tag, D>), grid, block, 0, ctx->stream, a, partials);
-    else
+    const dim3 block(kAttendThreads);
+    const dim3 grid = cut ? dim3(kWorkgroups) : dim3(static_cast<unsigned>(static_cast<int64_t>(a.t.n_seqs) * plan.n_blocks), d.n_kv_heads);
+    if constexpr (TILES > 1)
       hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, kQueryParts<Tag> == 1 ? (TILES == 4 ? 2 : 1) : 3>), grid, block, 0,
                          ctx->stream, a, partials);
+    else if (alone)
+      hipLaunchKernelGGL((attend_pages_kernel<Tag, D, 1>), grid, block, 0, ctx->stream, a, partials);
+    else
+      hipLaunchKernelGGL((attend_pages_kernel<Tag, D, kAttendWaves>), grid, block, 0, ctx->stream, a, partials);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (!cut) return hipSuccess;
   hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, TILES>), dim3(static_cast<unsigned>(items * TILES * kMergeSplit), d.n_kv_heads),
-                     dim3(kAttendThreads), 0, ctx->stream, t, plan, max_rows, d.n_q_heads, meta, partials, out, lse_out);
+                     dim3(kAttendThreads), 0, ctx->stream, t, plan, max_rows, d.n_q_heads, item_start, partials, out, lse_out);
   return hipGetLastError();
 }
 
@@ -714,17 +761,14 @@ hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTa
   if constexpr (kQueryParts<Tag> == 1) return run<Tag, D, 8>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
 }
 
-template <int D>
-size_t scratch_bytes(int n_kv_heads, bool bf16) {
-  const size_t few = std::max(Division<1>::scratch_bytes<D>(n_kv_heads), Division<4>::scratch_bytes<D>(n_kv_heads));
-  return bf16 ? std::max(few, Division<8>::scratch_bytes<D>(n_kv_heads)) : few;
-}
-
 }  // namespace
 
+// Two slots for each unit of the largest launch that is cut: wavefronts with one tile each, or workgroups with four or eight.
 size_t attend_matrix_scratch_bytes(const ifkv_ctx *ctx) {
-  const auto &d = ctx->desc;
-  return d.head_dim == 128 ? scratch_bytes<128>(d.n_kv_heads, d.dtype == IFKV_BF16) : scratch_bytes<64>(d.n_kv_heads, d.dtype == IFKV_BF16);
+  const bool wide = ctx->desc.head_dim == 128;
+  const size_t four = wide ? sizeof(Image<128, 4>) : sizeof(Image<64, 4>), eight = wide ? sizeof(Image<128, 8>) : sizeof(Image<64, 8>);
+  const size_t one = kAttendWaves * (wide ? sizeof(Image<128, 1>) : sizeof(Image<64, 1>));
+  return kTableBytes + 2 * kWorkgroups * std::max(one, ctx->desc.dtype == IFKV_BF16 ? eight : four);
 }
 
 hipError_t launch_attend_matrix(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int32_t max_rows, const void *q,
