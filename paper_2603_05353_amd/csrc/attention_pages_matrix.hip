@@ -17,6 +17,8 @@ namespace ifkv {
 
 namespace {
 
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.402823466e38f;
@@ -81,6 +83,7 @@ struct Columns {
   float ref[NT], neg_ref[NT], sum[NT];
   int pos[NT];          // INT32_MAX: sees nothing
   int64_t row_head[NT]; // -1: no row
+  uint32_t nan_mark[NT]; // outputs that saw a value that is NaN beside tokens that they do not see
   int lowest, highest;  // positions of the wavefront's columns that see something (INT32_MAX and -1: none does)
   int n, g;
 
@@ -133,6 +136,7 @@ struct Columns {
       ref[nt] = -INFINITY;
       neg_ref[nt] = 0.f;
       sum[nt] = 0.f;
+      nan_mark[nt] = 0;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt][nt] = f32x4{0, 0, 0, 0};
     }
@@ -165,8 +169,8 @@ struct Columns {
 
   __device__ __forceinline__ bool masked(int token0) const { return token0 + kPageTokens - 1 > lowest; }
 
-  // exponentials of a page's logits, as the second product takes them
-  __device__ __forceinline__ void weights(int token0, float logit_scale, f32x4 (&s)[4][NT], bf16x8 (&w)[2][NT][PP]) {
+  // masks a page's logits and sees to the references
+  __device__ __forceinline__ void prepare(int token0, float logit_scale, f32x4 (&s)[4][NT]) {
     if (masked(token0)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -206,97 +210,97 @@ struct Columns {
           for (int e = 0; e < 4; ++e) o[dt][nt][e] *= by;
       }
     }
+  }
+
+  // exponentials of half a page's logits, as the second product takes them
+  __device__ __forceinline__ void weights(int half, float logit_scale, const f32x4 (&s)[4][NT], bf16x8 (&w)[NT][PP]) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      float p[8];
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        float p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(s[2 * st + e / 4][nt][e % 4], logit_scale, neg_ref[nt]));
-          sum[nt] += p[e];
-        }
-        split8<PP>(p, w[st][nt]);
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(s[2 * half + e / 4][nt][e % 4], logit_scale, neg_ref[nt]));
+        sum[nt] += p[e];
       }
+      split8<PP>(p, w[nt]);
     }
   }
 
   // the bytes that are NaN, 1 in each
   static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7; }
 
-  // Values behind a column's token count nothing, NaN neither.  Where a page that has such tokens holds NaN at all, its NaN
-  // bytes are taken as zero by add_values (the answer is true), and columns that do see one become NaN here.
+  // Values behind a column's token count nothing, NaN neither.  Whether a page that has such tokens holds NaN; if so columns that do
+  // see one are marked, and the caller takes the NaN bytes for zero (`clean`).
   template <typename F>
-  __device__ __forceinline__ bool drop_nan(int token0, F values) {
+  __device__ __forceinline__ bool find_nan(int token0, F values) {
     uint32_t any = 0;
-#pragma unroll
+#pragma unroll 1   // (loops: a rare path must not take registers from the others)
     for (int dt = 0; dt < DT; ++dt) {
       const v4u v = values(dt);
 #pragma unroll
       for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F7F7F7Fu) + 0x01010101u;
-      if (dt % 2 == 1) __builtin_amdgcn_sched_barrier(0);
     }
     if (__ballot((any & 0x80808080u) != 0) == 0) return false;
+#pragma unroll 1
+    for (int dt = 0; dt < DT; ++dt) {
+      const v4u v = values(dt);
+      v4u one;   // 1.0 in e4m3 where there is a NaN
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int last = pos[nt] - token0 - g * 4;
-      bf16x8 seen[2];
+      for (int e = 0; e < 4; ++e) one[e] = nan_bytes(v[e]) * 0x38u;
 #pragma unroll
-      for (int st = 0; st < 2; ++st)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) seen[st][e] = static_cast<__bf16>((2 * st + e / 4) * 16 + e % 4 <= last ? 1.f : 0.f);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const v4u v = values(dt);
-        v4u one;   // 1.0 in e4m3 where there is a NaN
-#pragma unroll
-        for (int e = 0; e < 4; ++e) one[e] = nan_bytes(v[e]) * 0x38u;
+      for (int nt = 0; nt < NT; ++nt) {
+        const int last = pos[nt] - token0 - g * 4;
         f32x4 count = {0, 0, 0, 0};
-        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(one.x, one.y, 1.f), seen[0], count, 0, 0, 0);
-        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(one.z, one.w, 1.f), seen[1], count, 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (count[e] > 0.f) o[dt][nt][e] = __uint_as_float(0x7FC00000u);
-        __builtin_amdgcn_sched_barrier(0);   // one after the other: this path must not take registers from the others
+        for (int half = 0; half < 2; ++half) {
+          bf16x8 seen;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) seen[e] = static_cast<__bf16>((2 * half + e / 4) * 16 + e % 4 <= last ? 1.f : 0.f);
+          count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(one[2 * half], one[2 * half + 1], 1.f), seen, count, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) nan_mark[nt] |= count[e] > 0.f ? 1u << (dt * 4 + e) : 0u;
       }
     }
     return true;
   }
-
-  static __device__ __forceinline__ void clean(v4u &v) {
+  static __device__ __forceinline__ v4u clean(v4u v) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] &= ~(nan_bytes(v[e]) * 0xFFu);
-  }
-  template <bool CLEAN, typename F>
-  __device__ __forceinline__ void add(F values, float scale, const bf16x8 (&w)[2][NT][PP]) {
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      v4u v = values(dt);
-      if constexpr (CLEAN) clean(v);
-      const bf16x8 a0 = widen(v.x, v.y, scale), a1 = widen(v.z, v.w, scale);
-#pragma unroll
-      for (int p = PP - 1; p >= 0; --p)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w[0][nt][p], o[dt][nt], 0, 0, 0);
-          o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w[1][nt][p], o[dt][nt], 0, 0, 0);
-        }
-      if (CLEAN || (NT > 1 && dt % 4 == 3)) __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-  // values(dt): what this lane names of a page (value_offset)
-  template <typename F>
-  __device__ __forceinline__ void add_values(int token0, F values, float scale, const bf16x8 (&w)[2][NT][PP]) {
-    if (masked(token0) && drop_nan(token0, values))
-      add<true>(values, scale, w);
-    else
-      add<false>(values, scale, w);
+    return v;
   }
 
-  // a column's tokens are spread over four lanes
-  __device__ __forceinline__ void join_sums() {
+  // the second product: half a page after the other, so that the weights of one half are held at a time
+  // values(dt, half): eight bytes of what this lane names of a page (value_offset)
+  template <typename F>
+  __device__ __forceinline__ void add_values(F values, float scale, float logit_scale, const f32x4 (&s)[4][NT]) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      bf16x8 w[NT][PP];
+      weights(half, logit_scale, s, w);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const v2u v = values(dt, half);
+        const bf16x8 a = widen(v.x, v.y, scale);
+#pragma unroll
+        for (int p = PP - 1; p >= 0; --p)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[nt][p], o[dt][nt], 0, 0, 0);
+        if (NT > 1 && dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+
+  // after the last page: a column's tokens are spread over four lanes; columns that see nothing had queries of zero and no mask
+  __device__ __forceinline__ void complete() {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      if (pos[nt] == INT32_MAX) ref[nt] = -INFINITY;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (nan_mark[nt] >> (dt * 4 + e) & 1) o[dt][nt][e] = __uint_as_float(0x7FC00000u);
       sum[nt] += __shfl_xor(sum[nt], 16, 64);
       sum[nt] += __shfl_xor(sum[nt], 32, 64);
     }
@@ -317,13 +321,6 @@ struct Columns {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
       if (row_head[nt] >= 0) write_columns<Tag, D, DT>(out, lse_out, row_head[nt], 0, g, &o[0][nt], NT, ref[nt], sum[nt]);
-  }
-
-  // columns that see nothing had queries of zero and no mask
-  __device__ __forceinline__ void forget_unseen() {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-      if (pos[nt] == INT32_MAX) ref[nt] = -INFINITY;
   }
 };
 
@@ -378,22 +375,32 @@ __device__ __forceinline__ void each_piece(const AttendPlan &plan, int n_items, 
 // room for the keys and the values of one page; direct loads fill it, the next page's keys as soon as this page's have been
 // used, then its values, so half a page is always under way and no wavefront waits for another.
 // ---------------------------------------------------------------------------
-template <typename Tag, int D, int TEAM>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_kernel(AttendArgs a, Image<D, 1> *__restrict__ partials) {
+#ifndef FWL
+#define FWL 256
+#endif
+// wavefronts a SIMD that the registers leave
+template <typename Tag, int D, int NT>
+constexpr int kFewWaves = NT * kQueryParts<Tag> * D <= FWL || NT == 1 ? 2 : 1;
+
+template <typename Tag, int D, int NT, int TEAM>
+__global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void attend_pages_kernel(AttendArgs a, Image<D, NT> *__restrict__ partials) {
   constexpr int PP = kQueryParts<Tag> == 1 ? 2 : 3;
-  using Cols = Columns<Tag, D, 1, PP>;
+  using Cols = Columns<Tag, D, NT, PP>;
   constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
   constexpr int LOADS = TILE / 1024;   // of 1 KiB, for a page's keys or values
+#ifndef DEP
+#define DEP 1
+#endif
+  constexpr int DEPTH = NT == 1 ? 1 : DEP;   // pages that a wavefront has room for
   __shared__ AttendPlanMemory plan_memory;
   __shared__ union {
-    v4u tile[kAttendWaves][2][LOADS][64];
-    Image<D, 1> image[2];
+    v4u tile[kAttendWaves][DEPTH][2][LOADS][64];
+    Image<D, NT> image[2];
   } mem;
   const PageTable &t = a.t;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int key_lane = key_offset<D>(lane, 0, 0), value_lane = value_offset(lane, 0);
-  const v4u(*keys)[64] = mem.tile[wave][0], (*values)[64] = mem.tile[wave][1];
-  const uint32_t keys_at = lds_address(keys), values_at = lds_address(values);
+  const uint32_t room_at = lds_address(mem.tile[wave]);
   const int member = TEAM == 1 ? 0 : wave;   // of the wavefronts that share an item's pages
 
   const auto piece = [&](int index, int h, int first, int last, int slot) __attribute__((always_inline)) {
@@ -418,47 +425,66 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_kernel(AttendA
       auto page_at = [&](int i) __attribute__((always_inline)) {
         return (static_cast<int64_t>(__builtin_amdgcn_readlane(entry, i)) * a.n_kv_heads + h) * TILE;
       };
-      auto request_keys = [&](int64_t at) __attribute__((always_inline)) {
+      auto request_keys = [&](int64_t at, int room) __attribute__((always_inline)) {
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) dma16_base_once(a.k_pages + at + l / KV * 16 * D + l % KV * 64, key_lane, keys_at + l * 1024);
+        for (int l = 0; l < LOADS; ++l)
+          dma16_base_once(a.k_pages + at + l / KV * 16 * D + l % KV * 64, key_lane, room_at + room * 2 * TILE + l * 1024);
       };
-      auto request_values = [&](int64_t at) __attribute__((always_inline)) {
+      auto request_values = [&](int64_t at, int room) __attribute__((always_inline)) {
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l) dma16_base_once(a.v_pages + at + l * 16 * kPageTokens, value_lane, values_at + l * 1024);
+        for (int l = 0; l < LOADS; ++l)
+          dma16_base_once(a.v_pages + at + l * 16 * kPageTokens, value_lane, room_at + room * 2 * TILE + TILE + l * 1024);
       };
-      int i = __builtin_ctzll(todo);
-      wait_vmem<0>();   // (scales and queries: what follows counts its own requests)
-      request_keys(page_at(i));
-      request_values(page_at(i));
-      while (true) {
+      wait_vmem<0>();        // (scales and queries: what follows counts its own requests)
+      uint64_t ahead = todo; // pages that are not requested yet
+#pragma unroll
+      for (int room = 0; room < DEPTH; ++room) {
+        if (ahead == 0) break;
+        const int64_t at = page_at(__builtin_ctzll(ahead));
+        request_keys(at, room);
+        request_values(at, room);
+        ahead &= ahead - 1;
+      }
+      for (int room = 0; todo != 0; room = room + 1 == DEPTH ? 0 : room + 1) {
+        const int i = __builtin_ctzll(todo);
         todo &= todo - 1;
-        const bool more = todo != 0;
-        const int next = more ? __builtin_ctzll(todo) : i;
-        const int64_t next_at = page_at(next);
+        const bool more = ahead != 0;   // a page takes this one's place: then all other places are under way too
+        const int64_t next_at = page_at(more ? __builtin_ctzll(ahead) : i);
         const float ks_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_lane), i));
         const float vs_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_lane), i));
         const int token0 = (base + i * TEAM) * kPageTokens;
-        wait_vmem<LOADS>();         // the keys are there, the values on their way
-        f32x4 s[4][1];
+        const v4u(*keys)[64] = mem.tile[wave][room][0];
+        v4u(*values)[64] = mem.tile[wave][room][1];
+        // the keys are there; these values and what is behind them are on their way
+        if (more)
+          wait_vmem<(2 * DEPTH - 1) * LOADS>();
+        else
+          wait_vmem<LOADS>();
+        f32x4 s[4][NT];
         c.logits([&](int rt, int u) __attribute__((always_inline)) { return keys[rt * KV + u][lane]; }, ks_page, s);
         if (more) {
           wait_lds_reads();
-          request_keys(next_at);
+          request_keys(next_at, room);
         }
-        bf16x8 w[2][1][PP];
-        c.weights(token0, a.logit_scale, s, w);
+        c.prepare(token0, a.logit_scale, s);
         if (more)
-          wait_vmem<LOADS>();
+          wait_vmem<(2 * DEPTH - 1) * LOADS>();
         else
           wait_vmem<0>();
-        c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return values[dt][lane]; }, vs_page, w);
+        const auto value = [&](int dt) __attribute__((always_inline)) { return values[dt][lane]; };
+        const auto half_value = [&](int dt, int half) __attribute__((always_inline)) { return reinterpret_cast<const v2u *>(&values[dt][lane])[half]; };
+        if (c.masked(token0) && c.find_nan(token0, value))
+#pragma unroll 1
+          for (int dt = 0; dt < DT; ++dt) values[dt][lane] = Cols::clean(values[dt][lane]);
+        c.add_values(half_value, vs_page, a.logit_scale, s);
         wait_lds_reads();
-        if (!more) break;
-        request_values(next_at);
-        i = next;
+        if (more) {
+          request_values(next_at, room);
+          ahead &= ahead - 1;
+        }
       }
     }
-    c.join_sums();
+    c.complete();
     if constexpr (TEAM > 1) {
       // wavefronts 2 and 3 into 0 and 1, then 1 into 0
 #pragma unroll
@@ -467,23 +493,25 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_kernel(AttendA
         if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
         __syncthreads();
         if (wave < half) {
-          const Image<D, 1> &im = mem.image[wave];
-          const float other = im.ref[0][c.n], m = fmaxf(c.ref[0], other);
-          const float x = c.ref[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[0] - m);
-          const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
-          c.ref[0] = m;
-          c.sum[0] = c.sum[0] * x + im.sum[0][c.n] * y;
+          const Image<D, NT> &im = mem.image[wave];
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const f32x4 o = im.o[dt][lane];
+          for (int nt = 0; nt < NT; ++nt) {
+            const float other = im.ref[nt][c.n], m = fmaxf(c.ref[nt], other);
+            const float x = c.ref[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[nt] - m);
+            const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
+            c.ref[nt] = m;
+            c.sum[nt] = c.sum[nt] * x + im.sum[nt][c.n] * y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) c.o[dt][0][e] = c.o[dt][0][e] * x + o[e] * y;
+            for (int dt = 0; dt < DT; ++dt) {
+              const f32x4 o = im.o[dt * NT + nt][lane];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) c.o[dt][nt][e] = c.o[dt][nt][e] * x + o[e] * y;
+            }
           }
         }
       }
     }
     if (TEAM == 1 || wave == 0) {
-      c.forget_unseen();
       if (slot < 0)
         c.finish(a.out, a.lse_out);
       else
@@ -532,6 +560,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(A
     const AttendItem item(t, a.plan, a.max_rows, index);
     Cols c;
     c.start(t, item, item.block * a.plan.columns + wave * NT * 16, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
+    __syncthreads();   // (the piece before has been read)
+    if (lane == 0) s_count[wave] = c.lowest;
+    __syncthreads();
+    const int block_lowest = min(min(s_count[0], s_count[1]), min(s_count[2], s_count[3]));
     const int32_t *row_of_table = t.table + static_cast<int64_t>(item.seq) * t.width;
     for (int base = first; base < last; base += kPageList) {
       __syncthreads();   // (the list before has been read)
@@ -569,18 +601,27 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(A
         request(p + kStages - 1);
         const int4 e = s_entry[p];
         const int token0 = __builtin_amdgcn_readfirstlane(e.y) * kPageTokens;
+        v4u(*stage)[64] = s_stage[p % kStages];
+        const auto value = [&](int dt) __attribute__((always_inline)) { return stage[LOADS / 2 + dt][lane]; };
+        // every wavefront looks for NaN where any of them has tokens that it does not see: all find the same, and all have marked
+        // their columns when the page is cleaned
+        if (token0 + kPageTokens - 1 > block_lowest && c.find_nan(token0, value)) {
+          __syncthreads();
+          for (int l = LOADS / 2 + wave; l < LOADS; l += kAttendWaves) stage[l][lane] = Cols::clean(stage[l][lane]);
+          __syncthreads();
+        }
         if (token0 > c.highest) continue;
-        const v4u(*stage)[64] = s_stage[p % kStages];
         f32x4 s[4][NT];
         c.logits([&](int rt, int u) __attribute__((always_inline)) { return stage[rt * KV + u][lane]; }, __int_as_float(e.z), s);
-        bf16x8 w[2][NT][PP];
-        c.weights(token0, a.logit_scale, s, w);
-        c.add_values(token0, [&](int dt) __attribute__((always_inline)) { return stage[LOADS / 2 + dt][lane]; }, __int_as_float(e.w), w);
+        c.prepare(token0, a.logit_scale, s);
+        const auto half_value = [&](int dt, int half) __attribute__((always_inline)) {
+          return reinterpret_cast<const v2u *>(&stage[LOADS / 2 + dt][lane])[half];
+        };
+        c.add_values(half_value, __int_as_float(e.w), a.logit_scale, s);
       }
       wait_vmem<0>();   // nothing is under way into LDS that is given up or used again
     }
-    c.join_sums();
-    c.forget_unseen();
+    c.complete();
     if (slot < 0)
       c.finish(a.out, a.lse_out);
     else
@@ -696,16 +737,16 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
 
 constexpr size_t kTableBytes = (kMaxItems + 4) / 4 * 4 * sizeof(int);
 
-#ifndef UNITS1
-#define UNITS1 512
-#endif
 #ifndef TEAMRULE
-#define TEAMRULE (items * d.n_kv_heads >= 512)
+#define TEAMRULE (items * d.n_kv_heads >= 2048)
 #endif
 #ifndef LP
 #define LP 8
 #endif
-constexpr int kWorkgroups = UNITS1;     // what the chip holds at two a CU: all of them run at once and end together
+#ifndef WG2
+#define WG2 256
+#endif
+constexpr int kMostUnits = 512;
 constexpr int kLeastPages = LP;
 
 template <typename Tag, int D, int TILES>
@@ -721,7 +762,8 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
   // (pages are added up in 32 bits)
   const bool cut = t.width > kLeastPages && items <= kMaxItems && items * t.width < INT32_MAX / d.n_kv_heads;
   const bool alone = TILES == 1 && cut && TEAMRULE;
-  plan.units = !cut ? 0 : alone ? kWorkgroups * kAttendWaves : kWorkgroups;
+  const int workgroups = TILES == 1 ? 256 : TILES == 2 ? WG2 : TILES <= 4 ? 256 : 512;
+  plan.units = !cut ? 0 : alone ? workgroups * kAttendWaves : workgroups;
   int *item_start = static_cast<int *>(ctx->page_partials);
   Image<D, TILES> *partials = reinterpret_cast<Image<D, TILES> *>(static_cast<char *>(ctx->page_partials) + kTableBytes);
   // a grid has fewer than 2^32 threads: so many sequences a launch (all of them where items are cut)
@@ -735,14 +777,20 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
                           lse_out != nullptr ? lse_out + skip * d.n_q_heads : nullptr, item_start, q_stride, max_rows,
                           static_cast<int>(pages.n_pages), d.n_q_heads, d.n_kv_heads, ctx->sm_scale * kLog2e};
     const dim3 block(kAttendThreads);
-    const dim3 grid = cut ? dim3(kWorkgroups) : dim3(static_cast<unsigned>(static_cast<int64_t>(a.t.n_seqs) * plan.n_blocks), d.n_kv_heads);
-    if constexpr (TILES > 1)
-      hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, kQueryParts<Tag> == 1 ? (TILES == 4 ? 2 : 1) : 3>), grid, block, 0,
-                         ctx->stream, a, partials);
-    else if (alone)
-      hipLaunchKernelGGL((attend_pages_kernel<Tag, D, 1>), grid, block, 0, ctx->stream, a, partials);
-    else
-      hipLaunchKernelGGL((attend_pages_kernel<Tag, D, kAttendWaves>), grid, block, 0, ctx->stream, a, partials);
+    const dim3 grid = cut ? dim3(workgroups) : dim3(static_cast<unsigned>(static_cast<int64_t>(a.t.n_seqs) * plan.n_blocks), d.n_kv_heads);
+    if constexpr (TILES > 4) {
+      if (static_cast<int64_t>(max_rows) * plan.group <= 64)
+        hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, 2>), grid, block, 0, ctx->stream, a, partials);
+      else
+        hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, 1>), grid, block, 0, ctx->stream, a, partials);
+    } else if constexpr (TILES > 1) {
+      hipLaunchKernelGGL((attend_pages_kernel<Tag, D, TILES, kAttendWaves>), grid, block, 0, ctx->stream, a, partials);
+    } else {
+      if (alone)
+        hipLaunchKernelGGL((attend_pages_kernel<Tag, D, 1, 1>), grid, block, 0, ctx->stream, a, partials);
+      else
+        hipLaunchKernelGGL((attend_pages_kernel<Tag, D, 1, kAttendWaves>), grid, block, 0, ctx->stream, a, partials);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -757,18 +805,21 @@ hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTa
                        void *out, float *lse_out) {
   const int64_t columns = static_cast<int64_t>(max_rows) * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads);
   if (columns <= 16) return run<Tag, D, 1>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
-  if (columns <= 64 || kQueryParts<Tag> > 1) return run<Tag, D, 4>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
-  if constexpr (kQueryParts<Tag> == 1) return run<Tag, D, 8>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+  if (columns <= 32 || kQueryParts<Tag> > 1) return run<Tag, D, 2>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+  if constexpr (kQueryParts<Tag> == 1) {
+    if (columns <= 48) return run<Tag, D, 3>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+    return run<Tag, D, 8>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+  }
 }
 
 }  // namespace
 
-// Two slots for each unit of the largest launch that is cut: wavefronts with one tile each, or workgroups with four or eight.
+// Two slots for each unit of the largest launch that is cut.
 size_t attend_matrix_scratch_bytes(const ifkv_ctx *ctx) {
   const bool wide = ctx->desc.head_dim == 128;
-  const size_t four = wide ? sizeof(Image<128, 4>) : sizeof(Image<64, 4>), eight = wide ? sizeof(Image<128, 8>) : sizeof(Image<64, 8>);
-  const size_t one = kAttendWaves * (wide ? sizeof(Image<128, 1>) : sizeof(Image<64, 1>));
-  return kTableBytes + 2 * kWorkgroups * std::max(one, ctx->desc.dtype == IFKV_BF16 ? eight : four);
+  const size_t one = 256 * kAttendWaves * (wide ? sizeof(Image<128, 1>) : sizeof(Image<64, 1>));   // (also two to four tiles, a workgroup)
+  const size_t eight = 512 * (wide ? sizeof(Image<128, 8>) : sizeof(Image<64, 8>));
+  return kTableBytes + 2 * std::max(one, ctx->desc.dtype == IFKV_BF16 ? eight : one);
 }
 
 hipError_t launch_attend_matrix(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int32_t max_rows, const void *q,
