@@ -227,7 +227,8 @@ class Layer:
         self._native = None   # also while bind() records and after close(); a stage reads it once, another thread may be binding
         if marshal is not None:
             functions = (self._lib.ifkv_reposition_keys, self._lib.ifkv_reposition_score, self._lib.ifkv_score_tokens,
-                         self._lib.ifkv_select_topk, self._lib.ifkv_recompute_attention, self._lib.ifkv_splice_kv, self._lib.ifkv_rope_rows)
+                         self._lib.ifkv_select_topk, self._lib.ifkv_recompute_attention, self._lib.ifkv_splice_kv, self._lib.ifkv_rope_rows,
+                         self._lib.ifkv_rope_rows_axes, self._lib.ifkv_store_pages, self._lib.ifkv_attend_pages, self._lib.ifkv_copy_pages)
             self._native = marshal.Caller(self._ctx.value, dtype == "bf16", n_q_heads, n_kv_heads, head_dim, self.token_stride,
                                           self.head_stride, *(C.cast(f, C.c_void_p).value for f in functions))
 
@@ -527,6 +528,12 @@ class Layer:
     def rope_rows_axes(self, x: torch.Tensor, pos: torch.Tensor, axes: torch.Tensor) -> torch.Tensor:
         """In place; x [R, n_heads, d] (rows may be slices of wider ones), pos int32 [R, n_axes],
         axes int32 [d/2] on the CPU: the axis that turns each pair."""
+        native = self._native
+        if native is not None:
+            rc = native.rope_rows_axes(x, pos, axes)
+            if rc is not None:
+                self._check(rc)
+                return x
         if axes.device.type != "cpu" or axes.dtype != torch.int32 or tuple(axes.shape) != (self.head_dim // 2,) or not axes.is_contiguous():
             raise ValueError(f"axes: expected a contiguous int32 tensor [{self.head_dim // 2}] on the CPU, got {axes.dtype} {tuple(axes.shape)} on {axes.device}")
         if pos.dim() != 2:
@@ -541,6 +548,12 @@ class Layer:
                     row_pos: torch.Tensor, row_start: Optional[torch.Tensor] = None) -> None:
         """Rows k_new, v_new [R, H_kv, d] -> the pages that table int32 [S, W] gives their sequences.  kv_len int32 [S]: tokens held
         before.  row_start int32 [S + 1]: the rows of sequence s are row_start[s]..row_start[s+1]-1; None: one row a sequence."""
+        native = self._native
+        if native is not None:
+            rc = native.store_pages(pages, table, kv_len, k_new, v_new, row_pos, row_start)
+            if rc is not None:
+                self._check(rc)
+                return
         n = int(k_new.shape[0])
         tp, n_seqs, width, sp, pp = self._table(table, row_start, row_pos, n)
         (kp, ks), (vp, vs) = self._rows(k_new, "k_new", self.n_kv_heads), self._rows(v_new, "v_new", self.n_kv_heads, rows=n)
@@ -557,11 +570,17 @@ class Layer:
         if out is None:
             out = self._empty(n, self.n_q_heads, self.head_dim)
         lse = self._empty(n, self.n_q_heads, dtype=torch.float32) if return_lse else None
+        if max_rows is None:
+            max_rows = 1 if row_start is None else max(n, 1)
+        native = self._native
+        if native is not None:
+            rc = native.attend_pages(q, row_pos, pages, table, row_start, max_rows, out, lse)
+            if rc is not None:
+                self._check(rc)
+                return (out, lse) if return_lse else out
         tp, n_seqs, width, sp, pp = self._table(table, row_start, row_pos, n)
         qp, stride = self._rows(q, "q", self.n_q_heads)
         desc = self._pages(pages)
-        if max_rows is None:
-            max_rows = 1 if row_start is None else max(n, 1)
         self._invoke(self._lib.ifkv_attend_pages, self._ctx, C.byref(desc), tp, n_seqs, width, sp, int(max_rows), qp, stride, pp, n,
                      self._packed(out, "out", (self.n_q_heads, self.head_dim), rows=n),
                      self._packed(lse, "lse", (self.n_q_heads,), dtype=torch.float32, rows=n))
@@ -569,6 +588,12 @@ class Layer:
 
     def copy_pages(self, pages: PageCache, src: Union[torch.Tensor, Sequence[int]], dst: Union[torch.Tensor, Sequence[int]]) -> None:
         """Page dst[i] becomes page src[i]; the lists are the host's (a sequence, or an int32 tensor on the CPU)."""
+        native = self._native
+        if native is not None:
+            rc = native.copy_pages(pages, src, dst)
+            if rc is not None:
+                self._check(rc)
+                return
         lists = []
         for name, t in (("src", src), ("dst", dst)):
             if not isinstance(t, torch.Tensor):

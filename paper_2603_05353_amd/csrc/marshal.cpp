@@ -32,6 +32,11 @@ struct Caller {
   decltype(&ifkv_recompute_attention) recompute_attention;
   decltype(&ifkv_splice_kv) splice_kv;
   decltype(&ifkv_rope_rows) rope_rows;
+  // null where the caller does not bring them (then the calls refuse)
+  decltype(&ifkv_rope_rows_axes) rope_rows_axes;
+  decltype(&ifkv_store_pages) store_pages;
+  decltype(&ifkv_attend_pages) attend_pages;
+  decltype(&ifkv_copy_pages) copy_pages;
 };
 
 // A tensor's address if it is what the C call expects; `ok` is cleared otherwise.
@@ -50,6 +55,53 @@ struct Args {
     if (t == nullptr || t->dim() != 3 || t->size(0) < rows || t->size(1) != c->n_kv_heads || t->size(2) != c->head_dim) return refuse();
     if (t->size(0) > 1 && (t->stride(0) != c->token_stride || t->stride(1) != c->head_stride || t->stride(2) != 1)) return refuse();
     return t->data_ptr();
+  }
+  // rows [R, heads, d] whose heads lie packed, slices of wider rows among them; heads < 0: any number
+  void *strided(PyObject *o, const Caller *c, int64_t heads, int64_t rows, int64_t *stride) {
+    const at::Tensor *t = plain(o, c->dtype);
+    if (t == nullptr || t->dim() != 3 || t->size(2) != c->head_dim || (heads >= 0 && t->size(1) != heads) || (rows >= 0 && t->size(0) != rows))
+      return refuse();
+    const int64_t packed = t->size(1) * c->head_dim;
+    *stride = packed;
+    if (t->size(0) > 0 && (t->stride(2) != 1 || (t->size(1) > 1 && t->stride(1) != c->head_dim))) return refuse();
+    if (t->size(0) > 1) {
+      if (t->stride(0) < packed) return refuse();
+      *stride = t->stride(0);
+    }
+    return t->data_ptr();
+  }
+  // a tuple of the four tensors of a page cache
+  ifkv_page_cache pages(PyObject *o, const Caller *c) {
+    ifkv_page_cache p = {};
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) {
+      ok = false;
+      return p;
+    }
+    PyObject *k = PyTuple_GET_ITEM(o, 0);
+    p.n_pages = rows(k);
+    p.k = packed(k, at::kFloat8_e4m3fn, {c->n_kv_heads, IFKV_PAGE_TOKENS, c->head_dim}, 0);
+    p.v = same_rows(PyTuple_GET_ITEM(o, 1), at::kFloat8_e4m3fn, {c->n_kv_heads, c->head_dim, IFKV_PAGE_TOKENS}, p.n_pages);
+    p.k_scale = static_cast<float *>(same_rows(PyTuple_GET_ITEM(o, 2), at::kFloat, {c->n_kv_heads}, p.n_pages));
+    p.v_scale = static_cast<float *>(same_rows(PyTuple_GET_ITEM(o, 3), at::kFloat, {c->n_kv_heads}, p.n_pages));
+    return p;
+  }
+  // a page table [S, W]
+  const int32_t *table(PyObject *o, int64_t *n_seqs, int64_t *width) {
+    const at::Tensor *t = plain(o, at::kInt);
+    if (t == nullptr || t->dim() != 2 || !t->is_contiguous() || t->size(0) > std::numeric_limits<int32_t>::max() ||
+        t->size(1) > std::numeric_limits<int32_t>::max())
+      return static_cast<const int32_t *>(refuse());
+    *n_seqs = t->size(0);
+    *width = t->size(1);
+    return static_cast<const int32_t *>(t->data_ptr());
+  }
+  // int32 [n] on the CPU
+  const int32_t *host_list(PyObject *o, int64_t n) {
+    const at::Tensor *t = THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr;
+    if (t == nullptr || !t->has_storage() || t->layout() != at::kStrided || !t->is_cpu() || t->scalar_type() != at::kInt || t->dim() != 1 ||
+        t->size(0) != n || !t->is_contiguous())
+      return static_cast<const int32_t *>(refuse());
+    return static_cast<const int32_t *>(t->data_ptr());
   }
   // rows of any tensor
   int64_t rows(PyObject *o) {
@@ -89,6 +141,10 @@ struct Args {
   void *refuse() {
     ok = false;
     return nullptr;
+  }
+  void *same_rows(PyObject *o, at::ScalarType dtype, std::initializer_list<int64_t> tail, int64_t n) {
+    void *p = packed(o, dtype, tail, n);
+    return ok && THPVariable_Unpack(o).size(0) == n ? p : refuse();
   }
   const at::Tensor *plain(PyObject *o, at::ScalarType dtype) {
     if (!THPVariable_CheckExact(o)) return nullptr;
@@ -309,12 +365,98 @@ PyObject *call_rope_rows(PyObject *o, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// Caller(ctx, bf16, n_q_heads, n_kv_heads, head_dim, token_stride, head_stride, seven addresses in the order of the struct)
+// (x, pos, axes)
+PyObject *call_rope_rows_axes(PyObject *o, PyObject *const *a, Py_ssize_t n) {
+  Caller *self = reinterpret_cast<Caller *>(o);
+  if (n != 3) return wrong_count();
+  return guarded([&]() -> PyObject * {
+    Args x;
+    if (self->rope_rows_axes == nullptr || !THPVariable_CheckExact(a[1]) || THPVariable_Unpack(a[1]).dim() != 2) return none();
+    int64_t stride = 0;
+    void *t = x.strided(a[0], self, -1, -1, &stride);
+    if (!x.ok) return none();
+    const int64_t rows = x.rows(a[0]), heads = THPVariable_Unpack(a[0]).size(1), n_axes = THPVariable_Unpack(a[1]).size(1);
+    const int32_t *pos = static_cast<const int32_t *>(x.packed(a[1], at::kInt, {n_axes}, rows));
+    const int32_t *axes = x.host_list(a[2], self->head_dim / 2);
+    if (!x.ok || heads > kInt32 || n_axes > kInt32) return none();
+    return PyLong_FromLong(without_gil([&] {
+      return self->rope_rows_axes(self->ctx, t, pos, static_cast<int32_t>(n_axes), axes, rows, static_cast<int32_t>(heads), stride);
+    }));
+  });
+}
+
+// (pages, table, kv_len, k_new, v_new, row_pos, row_start)
+PyObject *call_store_pages(PyObject *o, PyObject *const *a, Py_ssize_t n) {
+  Caller *self = reinterpret_cast<Caller *>(o);
+  if (n != 7) return wrong_count();
+  return guarded([&]() -> PyObject * {
+    Args x;
+    if (self->store_pages == nullptr) return none();
+    const ifkv_page_cache pages = x.pages(a[0], self);
+    int64_t n_seqs = 0, width = 0, k_stride = 0, v_stride = 0;
+    const int32_t *table = x.table(a[1], &n_seqs, &width);
+    const int64_t rows = x.rows(a[3]);
+    if (!x.ok) return none();
+    const int32_t *kv_len = static_cast<const int32_t *>(x.packed(a[2], at::kInt, {}, n_seqs));
+    const void *k = x.strided(a[3], self, self->n_kv_heads, rows, &k_stride), *v = x.strided(a[4], self, self->n_kv_heads, rows, &v_stride);
+    const int32_t *pos = static_cast<const int32_t *>(x.packed(a[5], at::kInt, {}, rows));
+    const int32_t *start = a[6] == Py_None ? nullptr : static_cast<const int32_t *>(x.packed(a[6], at::kInt, {}, n_seqs + 1));
+    if (!x.ok) return none();
+    return PyLong_FromLong(without_gil([&] {
+      return self->store_pages(self->ctx, &pages, table, static_cast<int32_t>(n_seqs), static_cast<int32_t>(width), kv_len, start, pos, rows, k, v,
+                               k_stride, v_stride);
+    }));
+  });
+}
+
+// (q, row_pos, pages, table, row_start, max_rows, out, lse)
+PyObject *call_attend_pages(PyObject *o, PyObject *const *a, Py_ssize_t n) {
+  Caller *self = reinterpret_cast<Caller *>(o);
+  if (n != 8) return wrong_count();
+  return guarded([&]() -> PyObject * {
+    Args x;
+    if (self->attend_pages == nullptr) return none();
+    int64_t n_seqs = 0, width = 0, stride = 0;
+    const void *q = x.strided(a[0], self, self->n_q_heads, -1, &stride);
+    const ifkv_page_cache pages = x.pages(a[2], self);
+    const int32_t *table = x.table(a[3], &n_seqs, &width);
+    if (!x.ok) return none();
+    const int64_t rows = x.rows(a[0]);
+    const int32_t *pos = static_cast<const int32_t *>(x.packed(a[1], at::kInt, {}, rows));
+    const int32_t *start = a[4] == Py_None ? nullptr : static_cast<const int32_t *>(x.packed(a[4], at::kInt, {}, n_seqs + 1));
+    const int64_t max_rows = x.number(a[5], std::numeric_limits<int32_t>::min(), kInt32);
+    void *out = x.packed(a[6], self->dtype, {self->n_q_heads, self->head_dim}, rows);
+    float *lse = a[7] == Py_None ? nullptr : static_cast<float *>(x.packed(a[7], at::kFloat, {self->n_q_heads}, rows));
+    if (!x.ok) return none();
+    return PyLong_FromLong(without_gil([&] {
+      return self->attend_pages(self->ctx, &pages, table, static_cast<int32_t>(n_seqs), static_cast<int32_t>(width), start,
+                                static_cast<int32_t>(max_rows), q, stride, pos, rows, out, lse);
+    }));
+  });
+}
+
+// (pages, src, dst)
+PyObject *call_copy_pages(PyObject *o, PyObject *const *a, Py_ssize_t n) {
+  Caller *self = reinterpret_cast<Caller *>(o);
+  if (n != 3) return wrong_count();
+  return guarded([&]() -> PyObject * {
+    Args x;
+    if (self->copy_pages == nullptr) return none();
+    const ifkv_page_cache pages = x.pages(a[0], self);
+    const int64_t count = x.rows(a[1]);
+    const int32_t *src = x.host_list(a[1], count), *dst = x.host_list(a[2], count);
+    if (!x.ok) return none();
+    return PyLong_FromLong(without_gil([&] { return self->copy_pages(self->ctx, &pages, count, src, dst); }));
+  });
+}
+
+// Caller(ctx, bf16, n_q_heads, n_kv_heads, head_dim, token_stride, head_stride, seven or eleven addresses in the order of the struct)
 PyObject *caller_new(PyTypeObject *type, PyObject *args, PyObject *) {
-  unsigned long long p[8];
+  unsigned long long p[12] = {};
   int bf16;
   long long d[5];
-  if (!PyArg_ParseTuple(args, "KpLLLLLKKKKKKK", &p[0], &bf16, &d[0], &d[1], &d[2], &d[3], &d[4], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7]))
+  if (!PyArg_ParseTuple(args, "KpLLLLLKKKKKKK|KKKK", &p[0], &bf16, &d[0], &d[1], &d[2], &d[3], &d[4], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7],
+                        &p[8], &p[9], &p[10], &p[11]))
     return nullptr;
   PyObject *o = type->tp_alloc(type, 0);
   if (o == nullptr) return nullptr;
@@ -333,12 +475,17 @@ PyObject *caller_new(PyTypeObject *type, PyObject *args, PyObject *) {
   c->recompute_attention = reinterpret_cast<decltype(c->recompute_attention)>(p[5]);
   c->splice_kv = reinterpret_cast<decltype(c->splice_kv)>(p[6]);
   c->rope_rows = reinterpret_cast<decltype(c->rope_rows)>(p[7]);
+  c->rope_rows_axes = reinterpret_cast<decltype(c->rope_rows_axes)>(p[8]);
+  c->store_pages = reinterpret_cast<decltype(c->store_pages)>(p[9]);
+  c->attend_pages = reinterpret_cast<decltype(c->attend_pages)>(p[10]);
+  c->copy_pages = reinterpret_cast<decltype(c->copy_pages)>(p[11]);
   return o;
 }
 
 #define IFKV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(call_##name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {IFKV_METHOD(reposition_keys), IFKV_METHOD(reposition_score), IFKV_METHOD(score_tokens), IFKV_METHOD(select_topk),
-                          IFKV_METHOD(recompute_attention), IFKV_METHOD(splice_kv), IFKV_METHOD(rope_rows), {nullptr, nullptr, 0, nullptr}};
+                          IFKV_METHOD(recompute_attention), IFKV_METHOD(splice_kv), IFKV_METHOD(rope_rows), IFKV_METHOD(rope_rows_axes),
+                          IFKV_METHOD(store_pages), IFKV_METHOD(attend_pages), IFKV_METHOD(copy_pages), {nullptr, nullptr, 0, nullptr}};
 #undef IFKV_METHOD
 
 PyTypeObject kCallerType = {PyVarObject_HEAD_INIT(nullptr, 0)};
