@@ -16,7 +16,7 @@ constexpr int kMaxItems = 1024;       // of a launch that is cut along the cache
 
 // An item is a block of query columns (row, query head of the kv head) of one sequence; all kv heads have the same items.
 // All pages of all items, kv head after kv head, make one long list, which is cut into equal shares, one for each unit of the
-// launch (a workgroup or a wavefront): long sequences are spread over many units, short ones stay whole, and all units end
+// launch (a workgroup): long sequences are spread over many units, short ones stay whole, and all units end
 // together however uneven the lengths are.  Only the device knows those: every workgroup adds up the items' pages (their last
 // rows' positions) and finds its share by itself.
 struct AttendPlan {

@@ -375,43 +375,37 @@ __device__ __forceinline__ void each_piece(const AttendPlan &plan, int n_items, 
 // room for the keys and the values of one page; direct loads fill it, the next page's keys as soon as this page's have been
 // used, then its values, so half a page is always under way and no wavefront waits for another.
 // ---------------------------------------------------------------------------
-#ifndef FWL
-#define FWL 256
-#endif
 // wavefronts a SIMD that the registers leave
 template <typename Tag, int D, int NT>
-constexpr int kFewWaves = NT * kQueryParts<Tag> * D <= FWL || NT == 1 ? 2 : 1;
+constexpr int kFewWaves = NT * kQueryParts<Tag> * D <= 256 || NT == 1 ? 2 : 1;
 
-template <typename Tag, int D, int NT, int TEAM>
+template <typename Tag, int D, int NT>
 __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void attend_pages_kernel(AttendArgs a, Image<D, NT> *__restrict__ partials) {
   constexpr int PP = kQueryParts<Tag> == 1 ? 2 : 3;
   using Cols = Columns<Tag, D, NT, PP>;
   constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
   constexpr int LOADS = TILE / 1024;   // of 1 KiB, for a page's keys or values
-#ifndef DEP
-#define DEP 1
-#endif
-  constexpr int DEPTH = NT == 1 ? 1 : DEP;   // pages that a wavefront has room for
   __shared__ AttendPlanMemory plan_memory;
   __shared__ union {
-    v4u tile[kAttendWaves][DEPTH][2][LOADS][64];
+    v4u tile[kAttendWaves][2][LOADS][64];   // keys and values of a page
     Image<D, NT> image[2];
   } mem;
   const PageTable &t = a.t;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int key_lane = key_offset<D>(lane, 0, 0), value_lane = value_offset(lane, 0);
-  const uint32_t room_at = lds_address(mem.tile[wave]);
-  const int member = TEAM == 1 ? 0 : wave;   // of the wavefronts that share an item's pages
+  const v4u(*keys)[64] = mem.tile[wave][0];
+  v4u(*values)[64] = mem.tile[wave][1];
+  const uint32_t keys_at = lds_address(keys), values_at = lds_address(values);
 
   const auto piece = [&](int index, int h, int first, int last, int slot) __attribute__((always_inline)) {
     const AttendItem item(t, a.plan, a.max_rows, index);
     Cols c;
     c.start(t, item, item.block * a.plan.columns, a.plan.group, h, a.n_q_heads, a.q, a.q_stride);
-    if (c.highest < 0) last = first;
+    last = min(last, c.highest < 0 ? first : (c.highest >> 6) + 1);
     const int32_t *row_of_table = t.table + static_cast<int64_t>(item.seq) * t.width;
     // pages of this wavefront, 64 at a time: lane i knows the i-th
-    for (int base = first + member; base < last; base += 64 * TEAM) {
-      const int mine = base + lane * TEAM;
+    for (int base = first + wave; base < last; base += 64 * kAttendWaves) {
+      const int mine = base + lane * kAttendWaves;
       int entry = -1;
       if (mine < last) entry = row_of_table[mine];
       uint64_t todo = __ballot(entry >= 0 && entry < a.n_pages);
@@ -425,50 +419,36 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
       auto page_at = [&](int i) __attribute__((always_inline)) {
         return (static_cast<int64_t>(__builtin_amdgcn_readlane(entry, i)) * a.n_kv_heads + h) * TILE;
       };
-      auto request_keys = [&](int64_t at, int room) __attribute__((always_inline)) {
+      const auto request_keys = [&](int64_t at) __attribute__((always_inline)) {
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l)
-          dma16_base_once(a.k_pages + at + l / KV * 16 * D + l % KV * 64, key_lane, room_at + room * 2 * TILE + l * 1024);
+        for (int l = 0; l < LOADS; ++l) dma16_base_once(a.k_pages + at + l / KV * 16 * D + l % KV * 64, key_lane, keys_at + l * 1024);
       };
-      auto request_values = [&](int64_t at, int room) __attribute__((always_inline)) {
+      const auto request_values = [&](int64_t at) __attribute__((always_inline)) {
 #pragma unroll
-        for (int l = 0; l < LOADS; ++l)
-          dma16_base_once(a.v_pages + at + l * 16 * kPageTokens, value_lane, room_at + room * 2 * TILE + TILE + l * 1024);
+        for (int l = 0; l < LOADS; ++l) dma16_base_once(a.v_pages + at + l * 16 * kPageTokens, value_lane, values_at + l * 1024);
       };
-      wait_vmem<0>();        // (scales and queries: what follows counts its own requests)
-      uint64_t ahead = todo; // pages that are not requested yet
-#pragma unroll
-      for (int room = 0; room < DEPTH; ++room) {
-        if (ahead == 0) break;
-        const int64_t at = page_at(__builtin_ctzll(ahead));
-        request_keys(at, room);
-        request_values(at, room);
-        ahead &= ahead - 1;
-      }
-      for (int room = 0; todo != 0; room = room + 1 == DEPTH ? 0 : room + 1) {
-        const int i = __builtin_ctzll(todo);
+      int i = __builtin_ctzll(todo);
+      wait_vmem<0>();   // (scales and queries: what follows counts its own requests)
+      request_keys(page_at(i));
+      request_values(page_at(i));
+      while (true) {
         todo &= todo - 1;
-        const bool more = ahead != 0;   // a page takes this one's place: then all other places are under way too
-        const int64_t next_at = page_at(more ? __builtin_ctzll(ahead) : i);
+        const bool more = todo != 0;
+        const int next = more ? __builtin_ctzll(todo) : i;
+        const int64_t next_at = page_at(next);
         const float ks_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_lane), i));
         const float vs_page = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_lane), i));
-        const int token0 = (base + i * TEAM) * kPageTokens;
-        const v4u(*keys)[64] = mem.tile[wave][room][0];
-        v4u(*values)[64] = mem.tile[wave][room][1];
-        // the keys are there; these values and what is behind them are on their way
-        if (more)
-          wait_vmem<(2 * DEPTH - 1) * LOADS>();
-        else
-          wait_vmem<LOADS>();
+        const int token0 = (base + i * kAttendWaves) * kPageTokens;
+        wait_vmem<LOADS>();   // the keys are there, the values on their way
         f32x4 s[4][NT];
         c.logits([&](int rt, int u) __attribute__((always_inline)) { return keys[rt * KV + u][lane]; }, ks_page, s);
         if (more) {
           wait_lds_reads();
-          request_keys(next_at, room);
+          request_keys(next_at);
         }
         c.prepare(token0, a.logit_scale, s);
         if (more)
-          wait_vmem<(2 * DEPTH - 1) * LOADS>();
+          wait_vmem<LOADS>();
         else
           wait_vmem<0>();
         const auto value = [&](int dt) __attribute__((always_inline)) { return values[dt][lane]; };
@@ -478,55 +458,50 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
           for (int dt = 0; dt < DT; ++dt) values[dt][lane] = Cols::clean(values[dt][lane]);
         c.add_values(half_value, vs_page, a.logit_scale, s);
         wait_lds_reads();
-        if (more) {
-          request_values(next_at, room);
-          ahead &= ahead - 1;
-        }
+        if (!more) break;
+        request_values(next_at);
+        i = next;
       }
     }
     c.complete();
-    if constexpr (TEAM > 1) {
-      // wavefronts 2 and 3 into 0 and 1, then 1 into 0
+    // wavefronts 2 and 3 into 0 and 1, then 1 into 0
 #pragma unroll
-      for (int half = 2; half >= 1; half >>= 1) {
-        __syncthreads();   // (the tiles, or the images of the step before)
-        if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
-        __syncthreads();
-        if (wave < half) {
-          const Image<D, NT> &im = mem.image[wave];
+    for (int half = 2; half >= 1; half >>= 1) {
+      __syncthreads();   // (the tiles, or the images of the step before)
+      if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
+      __syncthreads();
+      if (wave < half) {
+        const Image<D, NT> &im = mem.image[wave];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const float other = im.ref[nt][c.n], m = fmaxf(c.ref[nt], other);
-            const float x = c.ref[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[nt] - m);
-            const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
-            c.ref[nt] = m;
-            c.sum[nt] = c.sum[nt] * x + im.sum[nt][c.n] * y;
+        for (int nt = 0; nt < NT; ++nt) {
+          const float other = im.ref[nt][c.n], m = fmaxf(c.ref[nt], other);
+          const float x = c.ref[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[nt] - m);
+          const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
+          c.ref[nt] = m;
+          c.sum[nt] = c.sum[nt] * x + im.sum[nt][c.n] * y;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-              const f32x4 o = im.o[dt * NT + nt][lane];
+          for (int dt = 0; dt < DT; ++dt) {
+            const f32x4 o = im.o[dt * NT + nt][lane];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) c.o[dt][nt][e] = c.o[dt][nt][e] * x + o[e] * y;
-            }
+            for (int e = 0; e < 4; ++e) c.o[dt][nt][e] = c.o[dt][nt][e] * x + o[e] * y;
           }
         }
       }
     }
-    if (TEAM == 1 || wave == 0) {
+    if (wave == 0) {
       if (slot < 0)
         c.finish(a.out, a.lse_out);
       else
         c.save(partials[slot], 0);
     }
-    if constexpr (TEAM > 1) __syncthreads();   // the images are given up
+    __syncthreads();   // the images are given up
   };
   if (a.plan.units == 0) {
-    const int lanes = item_lanes(a.plan, a.max_rows);
-    const int n = __builtin_amdgcn_readfirstlane(item_pages(t, a.plan, a.max_rows, blockIdx.x, lane & (lanes - 1), lanes));
-    if (n > 0) piece(blockIdx.x, blockIdx.y, 0, n, -1);
+    piece(blockIdx.x, blockIdx.y, 0, INT32_MAX, -1);
     return;
   }
   add_up_items(t, a.plan, a.max_rows, blockIdx.x == 0, a.item_start, plan_memory);
-  each_piece(a.plan, t.n_seqs * a.plan.n_blocks, a.n_kv_heads, plan_memory, TEAM == 1 ? blockIdx.x * kAttendWaves + wave : blockIdx.x, piece);
+  each_piece(a.plan, t.n_seqs * a.plan.n_blocks, a.n_kv_heads, plan_memory, blockIdx.x, piece);
 }
 
 // ---------------------------------------------------------------------------
@@ -737,17 +712,19 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
 
 constexpr size_t kTableBytes = (kMaxItems + 4) / 4 * 4 * sizeof(int);
 
-#ifndef TEAMRULE
-#define TEAMRULE (items * d.n_kv_heads >= 2048)
-#endif
-#ifndef LP
-#define LP 8
-#endif
-#ifndef WG2
-#define WG2 256
-#endif
-constexpr int kMostUnits = 512;
-constexpr int kLeastPages = LP;
+// The longest sequences, in pages, whose items are taken whole by a workgroup each.  Without cuts there is nothing to plan and to
+// join, 6 to 10 us less; what is lost is time at the end, when only the longest are left, and chips that are not full.  With a
+// workgroup for every CU or more, up to 64 pages (200 sequences of up to 1.5K tokens 72 us instead of 97, 32 of up to 2K 23
+// instead of 32; 64 of up to 8K, 128 pages, 141 instead of 109); otherwise up to 20 (one of 1000 tokens 10.6 us instead of 13.7, of
+// 2000 20 instead of 14).
+constexpr int kWholePages = 64, kWholePagesFewItems = 20, kManyItems = 256;
+
+// Workgroups of a launch that is cut: what the chip holds, so that all of them run at once and end together.  One a CU where
+// every wavefront has its own pages (with two a CU half the memory for partial results would be gone again on planning and
+// joining: one sequence of 130K tokens 55 instead of 52 us, 8 rows of 12 sequences 87 instead of 82), two a CU for blocks that share
+// pages (512 rows over 32K: 303 us, with one 497).
+constexpr int kTeams = 256, kBlockTeams = 512;
+constexpr int kLeastPages = kAttendWaves;   // of a unit: one for each wavefront
 
 template <typename Tag, int D, int TILES>
 hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int max_rows, const void *q, int64_t q_stride, void *out,
@@ -760,10 +737,9 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
   plan.least_pages = kLeastPages;
   const int64_t items = static_cast<int64_t>(t.n_seqs) * plan.n_blocks;
   // (pages are added up in 32 bits)
-  const bool cut = t.width > kLeastPages && items <= kMaxItems && items * t.width < INT32_MAX / d.n_kv_heads;
-  const bool alone = TILES == 1 && cut && TEAMRULE;
-  const int workgroups = TILES == 1 ? 256 : TILES == 2 ? WG2 : TILES <= 4 ? 256 : 512;
-  plan.units = !cut ? 0 : alone ? workgroups * kAttendWaves : workgroups;
+  const bool cut = t.width > (items * d.n_kv_heads >= kManyItems ? kWholePages : kWholePagesFewItems) && items <= kMaxItems && items * t.width < INT32_MAX / d.n_kv_heads;
+  const int workgroups = TILES <= 4 ? kTeams : kBlockTeams;
+  plan.units = cut ? workgroups : 0;
   int *item_start = static_cast<int *>(ctx->page_partials);
   Image<D, TILES> *partials = reinterpret_cast<Image<D, TILES> *>(static_cast<char *>(ctx->page_partials) + kTableBytes);
   // a grid has fewer than 2^32 threads: so many sequences a launch (all of them where items are cut)
@@ -783,13 +759,8 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
         hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, 2>), grid, block, 0, ctx->stream, a, partials);
       else
         hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, 1>), grid, block, 0, ctx->stream, a, partials);
-    } else if constexpr (TILES > 1) {
-      hipLaunchKernelGGL((attend_pages_kernel<Tag, D, TILES, kAttendWaves>), grid, block, 0, ctx->stream, a, partials);
     } else {
-      if (alone)
-        hipLaunchKernelGGL((attend_pages_kernel<Tag, D, 1, 1>), grid, block, 0, ctx->stream, a, partials);
-      else
-        hipLaunchKernelGGL((attend_pages_kernel<Tag, D, 1, kAttendWaves>), grid, block, 0, ctx->stream, a, partials);
+      hipLaunchKernelGGL((attend_pages_kernel<Tag, D, TILES>), grid, block, 0, ctx->stream, a, partials);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -817,9 +788,8 @@ hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTa
 // Two slots for each unit of the largest launch that is cut.
 size_t attend_matrix_scratch_bytes(const ifkv_ctx *ctx) {
   const bool wide = ctx->desc.head_dim == 128;
-  const size_t one = 256 * kAttendWaves * (wide ? sizeof(Image<128, 1>) : sizeof(Image<64, 1>));   // (also two to four tiles, a workgroup)
-  const size_t eight = 512 * (wide ? sizeof(Image<128, 8>) : sizeof(Image<64, 8>));
-  return kTableBytes + 2 * std::max(one, ctx->desc.dtype == IFKV_BF16 ? eight : one);
+  if (ctx->desc.dtype == IFKV_BF16) return kTableBytes + 2 * kBlockTeams * (wide ? sizeof(Image<128, 8>) : sizeof(Image<64, 8>));
+  return kTableBytes + 2 * kTeams * (wide ? sizeof(Image<128, 2>) : sizeof(Image<64, 2>));
 }
 
 hipError_t launch_attend_matrix(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int32_t max_rows, const void *q,
