@@ -78,6 +78,7 @@ struct Columns {
   static constexpr int KS = D / 32;       // steps of the first product
   static constexpr int KV = D / 64;       // 16-byte key loads of a lane and block of 16 tokens
   static constexpr int DT = D / 16;       // blocks of 16 output rows
+  static constexpr bool kFence = NT > 1;  // the order of requests and products is as written
   bf16x8 q[NT][QP][KS];
   f32x4 o[DT][NT];
   float ref[NT], neg_ref[NT], sum[NT];
@@ -144,26 +145,34 @@ struct Columns {
     highest = __builtin_amdgcn_readfirstlane(wave_max_i(highest));
   }
 
-  // keys(rt, u): what this lane names of a page (key_offset)
+  // keys.fetch(rt, i) requests, keys.open(., step) makes an operand, scaled, of what was fetched: kSteps steps each.  One block of
+  // 16 tokens is requested while the one before is worked on.
   template <typename F>
-  __device__ __forceinline__ void logits(F keys, float scale, f32x4 (&s)[4][NT]) {
+  __device__ __forceinline__ void logits(F keys, f32x4 (&s)[4][NT]) {
+    constexpr int N = KS / F::kSteps;
+    typename F::Word next[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) next[i] = keys.fetch(0, i);
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) {
+      typename F::Word now[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        now[i] = next[i];
+        if (rt < 3) next[i] = keys.fetch(rt + 1, i);
+      }
+      if (kFence) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) s[rt][nt] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int u = 0; u < KV; ++u) {
-        const v4u w = keys(rt, u);
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 a = keys.open(now[ks / F::kSteps], ks % F::kSteps);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const bf16x8 a = half == 0 ? widen(w.x, w.y, scale) : widen(w.z, w.w, scale);
+        for (int p = QP - 1; p >= 0; --p)   // smallest first
 #pragma unroll
-          for (int p = QP - 1; p >= 0; --p)   // smallest first
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              s[rt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nt][p][2 * u + half], s[rt][nt], 0, 0, 0);
-        }
+          for (int nt = 0; nt < NT; ++nt) s[rt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nt][p][ks], s[rt][nt], 0, 0, 0);
       }
+      if (kFence) __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -226,27 +235,13 @@ struct Columns {
     }
   }
 
-  // the bytes that are NaN, 1 in each
-  static __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7; }
-
-  // Values behind a column's token count nothing, NaN neither.  Whether a page that has such tokens holds NaN; if so columns that do
-  // see one are marked, and the caller takes the NaN bytes for zero (`clean`).
+  // Values behind a column's token count nothing, NaN neither.  For pages that have such tokens, and NaN: ones(dt, half) is 1 where a
+  // value is NaN; columns that see one are marked, and the caller takes those values for zero.
   template <typename F>
-  __device__ __forceinline__ bool find_nan(int token0, F values) {
-    uint32_t any = 0;
-#pragma unroll 1   // (loops: a rare path must not take registers from the others)
+  __device__ __forceinline__ void mark_nan(int token0, F ones) {
+#pragma unroll 1   // (a loop: a rare path must not take registers from the others)
     for (int dt = 0; dt < DT; ++dt) {
-      const v4u v = values(dt);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F7F7F7Fu) + 0x01010101u;
-    }
-    if (__ballot((any & 0x80808080u) != 0) == 0) return false;
-#pragma unroll 1
-    for (int dt = 0; dt < DT; ++dt) {
-      const v4u v = values(dt);
-      v4u one;   // 1.0 in e4m3 where there is a NaN
-#pragma unroll
-      for (int e = 0; e < 4; ++e) one[e] = nan_bytes(v[e]) * 0x38u;
+      const bf16x8 one[2] = {ones(dt, 0), ones(dt, 1)};
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int last = pos[nt] - token0 - g * 4;
@@ -256,38 +251,47 @@ struct Columns {
           bf16x8 seen;
 #pragma unroll
           for (int e = 0; e < 8; ++e) seen[e] = static_cast<__bf16>((2 * half + e / 4) * 16 + e % 4 <= last ? 1.f : 0.f);
-          count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(one[2 * half], one[2 * half + 1], 1.f), seen, count, 0, 0, 0);
+          count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one[half], seen, count, 0, 0, 0);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) nan_mark[nt] |= count[e] > 0.f ? 1u << (dt * 4 + e) : 0u;
       }
     }
-    return true;
-  }
-  static __device__ __forceinline__ v4u clean(v4u v) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] &= ~(nan_bytes(v[e]) * 0xFFu);
-    return v;
   }
 
   // the second product: half a page after the other, so that the weights of one half are held at a time
-  // values(dt, half): eight bytes of what this lane names of a page (value_offset)
+  // values.fetch(dt, half) requests, values.open makes the operand of a block of 16 output rows, scaled.  Four blocks are requested
+  // while the four before are worked on, the second half's exponentials are formed while the first half's products run.
   template <typename F>
-  __device__ __forceinline__ void add_values(F values, float scale, float logit_scale, const f32x4 (&s)[4][NT]) {
+  __device__ __forceinline__ void add_values(F values, float logit_scale, const f32x4 (&s)[4][NT]) {
+    constexpr int GROUPS = DT / 4;   // of a half
+    bf16x8 w[2][NT][PP];
+    typename F::Word next[4];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      bf16x8 w[NT][PP];
-      weights(half, logit_scale, s, w);
+    for (int i = 0; i < 4; ++i) next[i] = values.fetch(i, 0);
+    if (kFence) __builtin_amdgcn_sched_barrier(0);
+    weights(0, logit_scale, s, w[0]);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const v2u v = values(dt, half);
-        const bf16x8 a = widen(v.x, v.y, scale);
+    for (int j = 0; j < 2 * GROUPS; ++j) {
+      const int half = j / GROUPS, dt0 = j % GROUPS * 4;
+      typename F::Word now[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        now[i] = next[i];
+        if (j + 1 < 2 * GROUPS) next[i] = values.fetch((j + 1) % GROUPS * 4 + i, (j + 1) / GROUPS);
+      }
+      if (kFence) __builtin_amdgcn_sched_barrier(0);
+      if (j == GROUPS - 1) weights(1, logit_scale, s, w[1]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bf16x8 a = values.open(now[i]);
 #pragma unroll
         for (int p = PP - 1; p >= 0; --p)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) o[dt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[nt][p], o[dt][nt], 0, 0, 0);
-        if (NT > 1 && dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+          for (int nt = 0; nt < NT; ++nt)
+            o[dt0 + i][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[half][nt][p], o[dt0 + i][nt], 0, 0, 0);
       }
+      if (kFence) __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -322,6 +326,48 @@ struct Columns {
     for (int nt = 0; nt < NT; ++nt)
       if (row_head[nt] >= 0) write_columns<Tag, D, DT>(out, lse_out, row_head[nt], 0, g, &o[0][nt], NT, ref[nt], sum[nt]);
   }
+};
+
+// The e4m3 bytes of a word that are NaN, 1 in each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7; }
+// The bf16 halves of a word whose exponent is all ones, 1 in each.
+__device__ __forceinline__ uint32_t nan_halves(uint32_t w) { return (((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15; }
+
+// Operands from e4m3 bytes in LDS, in the order of the lanes.
+template <int KV>
+struct NarrowKeys {
+  static constexpr int kSteps = 2;
+  typedef v4u Word;
+  const v4u (*at)[64];
+  int lane;
+  float scale;
+  __device__ __forceinline__ v4u fetch(int rt, int i) const { return at[rt * KV + i][lane]; }
+  __device__ __forceinline__ bf16x8 open(const v4u &v, int step) const { return step == 0 ? widen(v.x, v.y, scale) : widen(v.z, v.w, scale); }
+};
+struct NarrowValues {
+  typedef v2u Word;
+  const v4u (*at)[64];
+  int lane;
+  float scale;
+  __device__ __forceinline__ v2u fetch(int dt, int half) const { return reinterpret_cast<const v2u *>(&at[dt][lane])[half]; }
+  __device__ __forceinline__ bf16x8 open(const v2u &v) const { return widen(v.x, v.y, scale); }
+};
+// Operands that are there.
+template <int KV>
+struct WideKeys {
+  static constexpr int kSteps = 1;
+  typedef v4u Word;
+  const v4u (*at)[2][64];
+  int lane;
+  __device__ __forceinline__ v4u fetch(int rt, int i) const { return at[rt * KV + i / 2][i % 2][lane]; }
+  __device__ __forceinline__ bf16x8 open(const v4u &v, int) const { return __builtin_bit_cast(bf16x8, v); }
+};
+struct WideValues {
+  typedef v4u Word;
+  const v4u (*at)[2][64];
+  int lane;
+  __device__ __forceinline__ v4u fetch(int dt, int half) const { return at[dt][half][lane]; }
+  __device__ __forceinline__ bf16x8 open(const v4u &v) const { return __builtin_bit_cast(bf16x8, v); }
 };
 
 struct AttendArgs {
@@ -441,7 +487,7 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
         const int token0 = (base + i * kAttendWaves) * kPageTokens;
         wait_vmem<LOADS>();   // the keys are there, the values on their way
         f32x4 s[4][NT];
-        c.logits([&](int rt, int u) __attribute__((always_inline)) { return keys[rt * KV + u][lane]; }, ks_page, s);
+        c.logits(NarrowKeys<KV>{keys, lane, ks_page}, s);
         if (more) {
           wait_lds_reads();
           request_keys(next_at);
@@ -451,12 +497,25 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
           wait_vmem<LOADS>();
         else
           wait_vmem<0>();
-        const auto value = [&](int dt) __attribute__((always_inline)) { return values[dt][lane]; };
-        const auto half_value = [&](int dt, int half) __attribute__((always_inline)) { return reinterpret_cast<const v2u *>(&values[dt][lane])[half]; };
-        if (c.masked(token0) && c.find_nan(token0, value))
+        if (c.masked(token0)) {
+          uint32_t any = 0;
 #pragma unroll 1
-          for (int dt = 0; dt < DT; ++dt) values[dt][lane] = Cols::clean(values[dt][lane]);
-        c.add_values(half_value, vs_page, a.logit_scale, s);
+          for (int dt = 0; dt < DT; ++dt)
+            for (int e = 0; e < 4; ++e) any |= nan_bytes(values[dt][lane][e]);
+          if (__ballot(any != 0) != 0) {
+            c.mark_nan(token0, [&](int dt, int half) __attribute__((always_inline)) {
+              const v4u v = values[dt][lane];
+              return widen(nan_bytes(v[2 * half]) * 0x38u, nan_bytes(v[2 * half + 1]) * 0x38u, 1.f);   // (0x38 is 1)
+            });
+#pragma unroll 1
+            for (int dt = 0; dt < DT; ++dt) {
+              v4u v = values[dt][lane];
+              for (int e = 0; e < 4; ++e) v[e] &= ~(nan_bytes(v[e]) * 0xFFu);
+              values[dt][lane] = v;
+            }
+          }
+        }
+        c.add_values(NarrowValues{values, lane, vs_page}, a.logit_scale, s);
         wait_lds_reads();
         if (!more) break;
         request_values(next_at);
@@ -505,20 +564,20 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
 }
 
 // ---------------------------------------------------------------------------
-// More columns: each of the four wavefronts has NT * 16 of its own and all of them go through the same pages, which direct
-// loads bring into LDS kStages - 1 ahead, in the order in which the lanes take them out again (no bank is asked twice).
+// More columns: each of the four wavefronts has NT * 16 of its own and all of them go through the same pages.  A page's
+// elements become bf16 once for all, a quarter by each wavefront, and lie in LDS in the order in which lanes take them for
+// operands (no bank is asked twice); two pages have room, one that is worked on and one that is filled, with a barrier between them.
 // ---------------------------------------------------------------------------
-constexpr int kStages = 4;
 constexpr int kPageList = kAttendThreads;   // pages whose places are looked up together
 
 template <typename Tag, int D, int NT, int PP>
 __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(AttendArgs a, Image<D, 4 * NT> *__restrict__ partials) {
   using Cols = Columns<Tag, D, NT, PP>;
-  constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
+  constexpr int KV = Cols::KV, DT = Cols::DT, KS = Cols::KS, TILE = kPageTokens * D;
   constexpr int LOADS = 2 * TILE / 1024;              // of 1 KiB, a page: keys first
   constexpr int MINE = LOADS / kAttendWaves;          // of a wavefront
   __shared__ AttendPlanMemory plan_memory;
-  __shared__ v4u s_stage[kStages][LOADS][64];
+  __shared__ v4u s_page[2][LOADS][2][64];             // each 16 bytes of a page are two operands
   __shared__ int4 s_entry[kPageList];                 // page, its place in the sequence, scales
   __shared__ int s_count[kAttendWaves];
   const PageTable &t = a.t;
@@ -529,7 +588,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(A
     const int l = wave * MINE + u;
     offset[u] = l < LOADS / 2 ? key_offset<D>(lane, l / KV, l % KV) : value_offset(lane, l - LOADS / 2);
   }
-  const uint8_t *pool = wave < kAttendWaves / 2 ? a.k_pages : a.v_pages;   // the first half of the loads are keys
+  const bool keys_mine = wave < kAttendWaves / 2;     // the first half of the loads are keys
+  const uint8_t *pool = keys_mine ? a.k_pages : a.v_pages;
 
   const auto piece = [&](int index, int h, int first, int last, int slot) __attribute__((always_inline)) {
     const AttendItem item(t, a.plan, a.max_rows, index);
@@ -559,42 +619,62 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(A
       }
       __syncthreads();
       if (n_list == 0) continue;
-      auto request = [&](int p) __attribute__((always_inline)) {   // (behind the end: the last page once more, so that counts stay the same)
+      v4u raw[MINE];   // this wavefront's quarter of the next page
+      const auto load = [&](int p) __attribute__((always_inline)) {   // (behind the end: the last page once more)
         const int page = s_entry[min(p, n_list - 1)].x;
         const uint8_t *src = pool + (static_cast<int64_t>(page) * a.n_kv_heads + h) * TILE;
 #pragma unroll
-        for (int u = 0; u < MINE; ++u) dma16(src + offset[u], lds_address(&s_stage[p % kStages][wave * MINE + u][0]));
+        for (int u = 0; u < MINE; ++u) raw[u] = *reinterpret_cast<const v4u *>(src + offset[u]);
       };
-      wait_vmem<0>();
+      const auto fill = [&](int p) __attribute__((always_inline)) {
+        const int4 e = s_entry[min(p, n_list - 1)];
+        const float scale = __int_as_float(keys_mine ? e.z : e.w);
 #pragma unroll
-      for (int p = 0; p < kStages - 1; ++p) request(p);
+        for (int u = 0; u < MINE; ++u) {
+          v4u(*to)[64] = s_page[p & 1][wave * MINE + u];
+          to[0][lane] = __builtin_bit_cast(v4u, widen(raw[u].x, raw[u].y, scale));
+          to[1][lane] = __builtin_bit_cast(v4u, widen(raw[u].z, raw[u].w, scale));
+        }
+      };
+      load(0);
+      fill(0);
+      load(1);
       for (int p = 0; p < n_list; ++p) {
-        wait_vmem<(kStages - 2) * MINE>();   // this wavefront's share of page p is there
-        wait_lds_reads();                    // and it has taken all it needs of page p - 1
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" : : : "memory");
-        request(p + kStages - 1);
-        const int4 e = s_entry[p];
-        const int token0 = __builtin_amdgcn_readfirstlane(e.y) * kPageTokens;
-        v4u(*stage)[64] = s_stage[p % kStages];
-        const auto value = [&](int dt) __attribute__((always_inline)) { return stage[LOADS / 2 + dt][lane]; };
+        __syncthreads();   // page p is there, and nobody reads page p - 1 any more
+        fill(p + 1);
+        load(p + 2);
+        asm volatile("" : : : "memory");   // (the requests go out here)
+        const int token0 = __builtin_amdgcn_readfirstlane(s_entry[p].y) * kPageTokens;
+        v4u(*page)[2][64] = s_page[p & 1];
         // every wavefront looks for NaN where any of them has tokens that it does not see: all find the same, and all have marked
         // their columns when the page is cleaned
-        if (token0 + kPageTokens - 1 > block_lowest && c.find_nan(token0, value)) {
-          __syncthreads();
-          for (int l = LOADS / 2 + wave; l < LOADS; l += kAttendWaves) stage[l][lane] = Cols::clean(stage[l][lane]);
-          __syncthreads();
+        if (token0 + kPageTokens - 1 > block_lowest) {
+          uint32_t any = 0;
+#pragma unroll 1
+          for (int l = LOADS; l < 2 * LOADS; ++l)
+            for (int e = 0; e < 4; ++e) any |= nan_halves(page[l / 2][l % 2][lane][e]);
+          if (__ballot(any != 0) != 0) {
+            c.mark_nan(token0, [&](int dt, int half) __attribute__((always_inline)) {
+              v4u v = page[LOADS / 2 + dt][half][lane];
+              for (int e = 0; e < 4; ++e) v[e] = nan_halves(v[e]) * 0x3F80u;   // 1 in bf16
+              return __builtin_bit_cast(bf16x8, v);
+            });
+            __syncthreads();
+#pragma unroll 1
+            for (int l = LOADS + wave; l < 2 * LOADS; l += kAttendWaves) {
+              v4u v = page[l / 2][l % 2][lane];
+              for (int e = 0; e < 4; ++e) v[e] &= ~(nan_halves(v[e]) * 0xFFFFu);
+              page[l / 2][l % 2][lane] = v;
+            }
+            __syncthreads();
+          }
         }
         if (token0 > c.highest) continue;
         f32x4 s[4][NT];
-        c.logits([&](int rt, int u) __attribute__((always_inline)) { return stage[rt * KV + u][lane]; }, __int_as_float(e.z), s);
+        c.logits(WideKeys<KV>{page, lane}, s);
         c.prepare(token0, a.logit_scale, s);
-        const auto half_value = [&](int dt, int half) __attribute__((always_inline)) {
-          return reinterpret_cast<const v2u *>(&stage[LOADS / 2 + dt][lane])[half];
-        };
-        c.add_values(half_value, __int_as_float(e.w), a.logit_scale, s);
+        c.add_values(WideValues{page + LOADS / 2, lane}, a.logit_scale, s);
       }
-      wait_vmem<0>();   // nothing is under way into LDS that is given up or used again
     }
     c.complete();
     if (slot < 0)
