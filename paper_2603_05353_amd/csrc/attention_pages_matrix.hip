@@ -72,13 +72,13 @@ __device__ __forceinline__ int value_offset(int lane, int dt) { return (dt * 16 
 
 // NT * 16 query columns of a wavefront and what it has added up for them.  Lane l holds column l % 16 of every tile; the four
 // lanes of a column share its reference, each has its own tokens' sum.
-template <typename Tag, int D, int NT, int PP>
+// FENCED: requests and products stay in the order in which they are written (where operands are not at hand for many at once).
+template <typename Tag, int D, int NT, int PP, bool FENCED>
 struct Columns {
   static constexpr int QP = kQueryParts<Tag>;
   static constexpr int KS = D / 32;       // steps of the first product
   static constexpr int KV = D / 64;       // 16-byte key loads of a lane and block of 16 tokens
   static constexpr int DT = D / 16;       // blocks of 16 output rows
-  static constexpr bool kFence = NT > 1;  // the order of requests and products is as written
   bf16x8 q[NT][QP][KS];
   f32x4 o[DT][NT];
   float ref[NT], neg_ref[NT], sum[NT];
@@ -161,7 +161,7 @@ struct Columns {
         now[i] = next[i];
         if (rt < 3) next[i] = keys.fetch(rt + 1, i);
       }
-      if (kFence) __builtin_amdgcn_sched_barrier(0);
+      if (FENCED) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) s[rt][nt] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -172,7 +172,7 @@ struct Columns {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) s[rt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nt][p][ks], s[rt][nt], 0, 0, 0);
       }
-      if (kFence) __builtin_amdgcn_sched_barrier(0);
+      if (FENCED) __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -269,7 +269,7 @@ struct Columns {
     typename F::Word next[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) next[i] = values.fetch(i, 0);
-    if (kFence) __builtin_amdgcn_sched_barrier(0);
+    if (FENCED) __builtin_amdgcn_sched_barrier(0);
     weights(0, logit_scale, s, w[0]);
 #pragma unroll
     for (int j = 0; j < 2 * GROUPS; ++j) {
@@ -280,7 +280,7 @@ struct Columns {
         now[i] = next[i];
         if (j + 1 < 2 * GROUPS) next[i] = values.fetch((j + 1) % GROUPS * 4 + i, (j + 1) / GROUPS);
       }
-      if (kFence) __builtin_amdgcn_sched_barrier(0);
+      if (FENCED) __builtin_amdgcn_sched_barrier(0);
       if (j == GROUPS - 1) weights(1, logit_scale, s, w[1]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -291,14 +291,14 @@ struct Columns {
           for (int nt = 0; nt < NT; ++nt)
             o[dt0 + i][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[half][nt][p], o[dt0 + i][nt], 0, 0, 0);
       }
-      if (kFence && j == GROUPS - 1) {   // after every product six of the exponentials' instructions
+      if (FENCED && j == GROUPS - 1) {   // after every product six of the exponentials' instructions
 #pragma unroll
         for (int k = 0; k < 4 * NT * PP; ++k) {
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);
         }
       }
-      if (kFence) __builtin_amdgcn_sched_barrier(0);
+      if (FENCED) __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -435,7 +435,7 @@ constexpr int kFewWaves = NT * kQueryParts<Tag> * D <= 256 || NT == 1 ? 2 : 1;
 template <typename Tag, int D, int NT>
 __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void attend_pages_kernel(AttendArgs a, Image<D, NT> *__restrict__ partials) {
   constexpr int PP = kQueryParts<Tag> == 1 ? 2 : 3;
-  using Cols = Columns<Tag, D, NT, PP>;
+  using Cols = Columns<Tag, D, NT, PP, (NT > 1)>;
   constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
   constexpr int LOADS = TILE / 1024;   // of 1 KiB, for a page's keys or values
   __shared__ AttendPlanMemory plan_memory;
@@ -579,7 +579,7 @@ constexpr int kPageList = kAttendThreads;   // pages whose places are looked up 
 
 template <typename Tag, int D, int NT, int PP>
 __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(AttendArgs a, Image<D, 4 * NT> *__restrict__ partials) {
-  using Cols = Columns<Tag, D, NT, PP>;
+  using Cols = Columns<Tag, D, NT, PP, true>;
   constexpr int KV = Cols::KV, DT = Cols::DT, KS = Cols::KS, TILE = kPageTokens * D;
   constexpr int LOADS = 2 * TILE / 1024;              // of 1 KiB, a page: keys first
   constexpr int MINE = LOADS / kAttendWaves;          // of a wavefront
@@ -831,7 +831,7 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
   const int64_t items = static_cast<int64_t>(t.n_seqs) * plan.n_blocks;
   // (pages are added up in 32 bits)
   const bool cut = t.width > (items * d.n_kv_heads >= kManyItems ? kWholePages : kWholePagesFewItems) && items <= kMaxItems && items * t.width < INT32_MAX / d.n_kv_heads;
-  const int workgroups = TILES <= 4 ? kTeams : kBlockTeams;
+  const int workgroups = TILES < 4 ? kTeams : kBlockTeams;
   plan.units = cut ? workgroups : 0;
   int *item_start = static_cast<int *>(ctx->page_partials);
   Image<D, TILES> *partials = reinterpret_cast<Image<D, TILES> *>(static_cast<char *>(ctx->page_partials) + kTableBytes);
@@ -847,11 +847,8 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
                           static_cast<int>(pages.n_pages), d.n_q_heads, d.n_kv_heads, ctx->sm_scale * kLog2e};
     const dim3 block(kAttendThreads);
     const dim3 grid = cut ? dim3(workgroups) : dim3(static_cast<unsigned>(static_cast<int64_t>(a.t.n_seqs) * plan.n_blocks), d.n_kv_heads);
-    if constexpr (TILES > 4) {
-      if (static_cast<int64_t>(max_rows) * plan.group <= 64)
-        hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, 2>), grid, block, 0, ctx->stream, a, partials);
-      else
-        hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, 1>), grid, block, 0, ctx->stream, a, partials);
+    if constexpr (TILES >= 4) {
+      hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, TILES == 4 ? 2 : 1>), grid, block, 0, ctx->stream, a, partials);
     } else {
       hipLaunchKernelGGL((attend_pages_kernel<Tag, D, TILES>), grid, block, 0, ctx->stream, a, partials);
     }
@@ -868,10 +865,14 @@ template <typename Tag, int D>
 hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int max_rows, const void *q, int64_t q_stride,
                        void *out, float *lse_out) {
   const int64_t columns = static_cast<int64_t>(max_rows) * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads);
+  // A wavefront with all columns converts a page's elements itself, alone and at its own pace; from four tiles on its registers do not
+  // suffice, and blocks share the pages (12 sequences of up to 20K: 35 columns 62 us, as a block 65; 64 columns as a block 116).
   if (columns <= 16) return run<Tag, D, 1>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if (columns <= 32 || kQueryParts<Tag> > 1) return run<Tag, D, 2>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if constexpr (kQueryParts<Tag> == 1) {
     if (columns <= 48) return run<Tag, D, 3>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+    // probabilities as two bf16 numbers; from here on the matrix cores bound the call, not memory, and one has to do
+    if (columns <= 64) return run<Tag, D, 4>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
     return run<Tag, D, 8>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   }
 }
