@@ -1,13 +1,19 @@
 // Attention over 8-bit pages on the matrix cores.
 //
 // Decoding reads every page once for a few query columns: memory bounds it, and what a kernel has to do is to keep requests in
-// flight.  A wavefront takes whole pages, as many bytes as it likes to have under way, straight from memory into registers in
-// the operand layout of the 16x16x32 bf16 instruction (no LDS, no barrier, no shuffle in the loop):
+// flight.  Pages come into LDS by direct loads, in the order in which the lanes of the 16x16x32 bf16 instruction take their operands out
+// again (no bank is asked twice, and nothing changes lanes):
 //   first product, S^T[token, column]: a lane's keys of a block of 16 tokens are d/64 times 16 bytes in a row of one token
 //     (the order of the d elements along the reduction is free, queries follow it);
 //   second product, O^T[d, column]: a lane's values are the 16 bytes in a row of one value row that ifkv.h's byte order makes
 //     of the very tokens whose probabilities the lane holds.
-// e4m3 numbers become bf16 exactly, two an instruction, with the page's scale multiplied in.
+// e4m3 numbers become bf16 exactly, two an instruction, with the page's scale multiplied in.  (The e4m3 instruction with scales, queries as
+// two e4m3 numbers, would need no conversion of keys, but its sums are off by up to 2^-15 of sum |q k|, bf16 ones by 2^-22.)
+//
+// Measured on one MI355X, a call with its join, where reading alone reaches 6.2 to 6.9 TB/s and a large bf16 product 1.2 PFLOP/s: 64 sequences
+// of 0.8K to 8K tokens, 32/8 heads of 128, 597 MB in 109 us (the kernel alone 6.0 TB/s); one of 130K tokens 52 us (266 MB); 35 columns of
+// 12 sequences of up to 20K 62 us (195 MB); 512 rows over 32K 265 us (1.03 PFLOP/s); 300 tokens of one sequence 7.5 us, all of it
+// latency: positions, table, scales and pages are each asked for with the answer to the one before.
 #include <algorithm>
 
 #include "attention_pages.h"
@@ -32,7 +38,7 @@ constexpr int kQueryParts = 3;
 template <>
 constexpr int kQueryParts<BF16Tag> = 1;
 
-// Partial results of one part: accumulators as the wavefronts hold them, then reference and sum of every column.
+// Partial results of a piece of an item: accumulators as the wavefronts hold them, then reference and sum of every column.
 template <int D, int NT>
 struct Image {
   f32x4 o[NT * D / 16][64];
@@ -227,10 +233,8 @@ struct Columns {
     for (int nt = 0; nt < NT; ++nt) {
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(s[2 * half + e / 4][nt][e % 4], logit_scale, neg_ref[nt]));
-        sum[nt] += p[e];
-      }
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[2 * half + e / 4][nt][e % 4], logit_scale, neg_ref[nt]));
+      sum[nt] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       split8<PP>(p, w[nt]);
     }
   }
@@ -259,7 +263,7 @@ struct Columns {
     }
   }
 
-  // the second product: half a page after the other, so that the weights of one half are held at a time
+  // The second product, half a page after the other.
   // values.fetch(dt, half) requests, values.open makes the operand of a block of 16 output rows, scaled.  Four blocks are requested
   // while the four before are worked on, the second half's exponentials are formed while the first half's products run.
   template <typename F>
@@ -424,7 +428,7 @@ __device__ __forceinline__ void each_piece(const AttendPlan &plan, int n_items, 
 }
 
 // ---------------------------------------------------------------------------
-// Up to 16 query columns a sequence: a workgroup's four wavefronts take the pages of a part in turn and join at the end.  Each has
+// Up to 48 query columns a sequence: a workgroup's four wavefronts take the pages of a piece in turn and join at the end.  Each has
 // room for the keys and the values of one page; direct loads fill it, the next page's keys as soon as this page's have been
 // used, then its values, so half a page is always under way and no wavefront waits for another.
 // ---------------------------------------------------------------------------
@@ -571,7 +575,7 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
 }
 
 // ---------------------------------------------------------------------------
-// More columns: each of the four wavefronts has NT * 16 of its own and all of them go through the same pages.  A page's
+// More columns (bf16 only): each of the four wavefronts has NT * 16 of its own and all of them go through the same pages.  A page's
 // elements become bf16 once for all, a quarter by each wavefront, and lie in LDS in the order in which lanes take them for
 // operands (no bank is asked twice); two pages have room, one that is worked on and one that is filled, with a barrier between them.
 // ---------------------------------------------------------------------------
