@@ -30,12 +30,24 @@ __device__ __forceinline__ float scale_for(uint32_t amax_bits) {
   return __uint_as_float(static_cast<uint32_t>(max(e, 127 - 100)) << 23);
 }
 
-// Which sequence owns row r: the number of starts at or below it, counted by every wavefront for itself.
-__device__ __forceinline__ int sequence_of(const PageTable &t, int r) {
-  if (t.row_start == nullptr) return r;
-  int n = 0;
-  for (int s = threadIdx.x & 63; s < t.n_seqs; s += 64) n += t.row_start[s] <= r;
-  return wave_sum_i(n) - 1;
+// The sequence that owns row r and its rows, found by every wavefront for itself: the number of starts at or below r, less one
+// (-1 and n_seqs: none does), the largest of those and the smallest of the others.
+__device__ __forceinline__ int sequence_of(const PageTable &t, int r, int &lo, int &hi) {
+  if (t.row_start == nullptr) {
+    lo = r;
+    hi = r + 1;
+    return r;
+  }
+  int n = 0, below = 0, above = static_cast<int>(t.n_rows);
+  for (int s = threadIdx.x & 63; s <= t.n_seqs; s += 64) {
+    const int start = t.row_start[s];
+    n += start <= r;
+    below = start <= r ? max(below, start) : below;
+    above = start <= r ? above : min(above, start);
+  }
+  lo = wave_max_i(below);
+  hi = wave_min_i(above);
+  return wave_reduce_i(n, [](int a, int b) __attribute__((always_inline)) { return a + b; }) - 1;
 }
 
 // Bits of all lanes, or-ed.
@@ -54,14 +66,14 @@ __device__ __forceinline__ uint64_t wave_or(uint64_t v) {
 // token's key, or of four neighbouring tokens' values, which are four neighbouring bytes.  Which slots are filled is one
 // 64-bit mask (rows ascend: the row of a slot is the number of filled slots before it), so the only thing that the wavefronts
 // have to agree on is the largest element.  Memory bounds a finished context (32K tokens, 8 heads of 128 in bf16: 201 MB in
-// 41 us at a copy's rate), the chain positions -> rows -> scale -> bytes a single token.
+// 47 us, 41 at a copy's rate), the chain positions -> rows -> scale -> bytes a single token (one
+// of each of 64 sequences 7 us; of 512 36 us, where a token's values change 4 bytes of 128 cache lines a head).
 // ---------------------------------------------------------------------------
 template <typename Tag, int D>
-__global__ __launch_bounds__(kThreads) void store_pages_kernel(PageTable t, const int32_t *__restrict__ kv_len, uint8_t *__restrict__ k_pages,
-                                                               uint8_t *__restrict__ v_pages, float *__restrict__ k_scale,
-                                                               float *__restrict__ v_scale, int n_pages, int n_kv_heads,
-                                                               const char *__restrict__ k_new, const char *__restrict__ v_new,
-                                                               int64_t k_row_bytes, int64_t v_row_bytes, int rows_per_block) {
+__global__ __launch_bounds__(kThreads, Elem<Tag>::kBytes == 2 ? 5 : 4) void store_pages_kernel(
+    PageTable t, const int32_t *__restrict__ kv_len, uint8_t *__restrict__ k_pages, uint8_t *__restrict__ v_pages,
+    float *__restrict__ k_scale, float *__restrict__ v_scale, int n_pages, int n_kv_heads, const char *__restrict__ k_new,
+    const char *__restrict__ v_new, int64_t k_row_bytes, int64_t v_row_bytes, int rows_per_block) {
   using E = Elem<Tag>;
   constexpr int VE = E::kVec;
   constexpr int VECS = D / VE;                                              // 16-byte vectors of a row's head
@@ -79,25 +91,36 @@ __global__ __launch_bounds__(kThreads) void store_pages_kernel(PageTable t, cons
 
   const int r0 = static_cast<int>(blockIdx.x) * rows_per_block;
   const int r1 = static_cast<int>(min(static_cast<int64_t>(r0) + rows_per_block, t.n_rows));
-  int seq = __builtin_amdgcn_readfirstlane(sequence_of(t, r0));
-  int lo = 0, hi = 0, turn = 0;
-  if (seq >= 0) rows_of(t, seq, lo, hi);
+  const auto block_of = [&](int pos) __attribute__((always_inline)) { return pos >= 0 && (pos >> 6) < t.width ? pos >> 6 : -1; };
+  int seq = -1, lo = 0, hi = 0, turn = 0;
   for (int r = r0; r < r1;) {
-    while (r >= hi || seq < 0) {  // on to the row's sequence (sequences without rows are passed over)
+    // positions of the next rows (asked for before it is known whose they are) and of the one before them
+    const int ahead = t.row_pos[min(static_cast<int64_t>(r) + lane, t.n_rows - 1)], behind = t.row_pos[max(r - 1, 0)];
+    if (r == r0) {
+      seq = sequence_of(t, r0, lo, hi);
+      if (seq < 0) hi = 0;
+    }
+    while (r >= hi) {   // on to the row's sequence (sequences without rows are passed over)
       if (++seq >= t.n_seqs) return;
       rows_of(t, seq, lo, hi);
-      if (r < lo) r = lo;
-      if (r >= r1) return;
     }
-    const int rl = r + lane;
-    const int pl = rl < hi ? t.row_pos[rl] : -1;
-    const int before = r > lo ? t.row_pos[r - 1] : -1;
-    const int pos = __builtin_amdgcn_readfirstlane(pl);
-    const int logical = pos >> 6;
-    if (pos < 0 || logical >= t.width || (before >= 0 && (before >> 6) == logical)) {
-      ++r;  // no token, or a row of a page that began before
+    if (seq >= t.n_seqs) return;
+    if (r < lo) {
+      r = lo;
       continue;
     }
+    // the next row that is the first of its page
+    const int pl = lane < hi - r ? ahead : -1;
+    const int mine = block_of(pl);
+    int before = __shfl_up(mine, 1, 64);
+    if (lane == 0) before = r > lo ? block_of(behind) : -1;
+    const uint64_t begins = __ballot(mine >= 0 && mine != before && lane < r1 - r);
+    const int skip = begins != 0 ? __builtin_ctzll(begins) : 64;
+    if (skip > 0) {
+      r += min(skip, hi - r);
+      continue;
+    }
+    const int logical = __builtin_amdgcn_readfirstlane(mine);
     // (requests that need no other's answer go out together: the page, the length, the rows)
     const int page = page_of(t, seq, logical, n_pages);
     const int len = kv_len[seq];
@@ -216,7 +239,8 @@ __global__ __launch_bounds__(kThreads) void store_pages_kernel(PageTable t, cons
           uint32_t beside = there[u][e];
           if (back != 1.f && kept && has != 15) beside = rescale_e4m3(has == 0 ? *to : beside, back);
           const int s = e % 4 * 8;
-          const uint32_t fresh = (w[0][e / 4] >> s & 0xFF) | (w[1][e / 4] >> s & 0xFF) << 8 | (w[2][e / 4] >> s & 0xFF) << 16 | (w[3][e / 4] >> s & 0xFF) << 24;
+          const uint32_t fresh = (w[0][e / 4] >> s & 0xFF) | (w[1][e / 4] >> s & 0xFF) << 8 | (w[2][e / 4] >> s & 0xFF) << 16 |
+                                 (w[3][e / 4] >> s & 0xFF) << 24;
           *to = (beside & ~bytes) | (fresh & bytes);
         }
       }
@@ -257,9 +281,13 @@ __global__ __launch_bounds__(kThreads) void copy_pages_kernel(PagePairs pairs, c
 hipError_t launch_store_pages(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, const int32_t *kv_len, const void *k_new,
                               const void *v_new, int64_t k_stride, int64_t v_stride) {
   const auto &d = ctx->desc;
-  // rows a workgroup looks at: a page's worth where that still leaves the chip enough of them, fewer otherwise
-  const int64_t rows_per_block =
-      std::max<int64_t>({std::min<int64_t>(64, t.n_rows * d.n_kv_heads / 1024), (t.n_rows + (int64_t(1) << 20) - 1) >> 20, 1});
+  // Rows a workgroup looks at: a page's worth, or as few as make some 2048 workgroups of them.  Fewer are better where rows are dense (most
+  // workgroups find no page of their own), more where many pages get a row each: 512 workgroups for 64 sequences of 64 rows take 15 us,
+  // for 63 single rows and 2048 of a prompt 176; 2048 take 23 and 56.  The rows of one sequence alone are dense more often than
+  // not: 1024 (2048 rows of a prompt 8.4 us with 1024, 14.9 with 2048; 512 rows of as many pages 38 and 34).
+  const int64_t workgroups = t.n_seqs == 1 ? 1024 : 2048;
+  const int64_t rows_per_block = std::max<int64_t>(
+      {std::min<int64_t>(64, t.n_rows * d.n_kv_heads * 2 / workgroups), (t.n_rows + (int64_t(1) << 20) - 1) >> 20, 1});
   const int64_t e = static_cast<int64_t>(dtype_size(d.dtype));
   dim3 grid(static_cast<unsigned>((t.n_rows + rows_per_block - 1) / rows_per_block), d.n_kv_heads, 2), block(kThreads);
 #define IFKV_LAUNCH_STORE(TAG, D)                                                                                                      \
