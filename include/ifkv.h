@@ -375,7 +375,7 @@ int ifkv_reorder_chunks(ifkv_ctx *ctx, int32_t n_chunks, const int32_t *order_in
  *   axis_of_pair host int32 [d/2], each in [0, n_axes); read before the call returns
  *   row_stride   elements between rows, at least n_heads * d, a multiple of 16 bytes' worth; 0 = packed
  * Errors: IFKV_EINVAL for NULL pointers, negative sizes, an axis out of range, misaligned x,
- * a stride that does not fit.
+ * a stride that does not fit; IFKV_ESHAPE if n_rows or n_heads * d reach 2^31.
  */
 #define IFKV_MAX_AXES 8
 int ifkv_rope_rows_axes(ifkv_ctx *ctx, void *x, const int32_t *pos, int32_t n_axes, const int32_t *axis_of_pair,
@@ -467,6 +467,8 @@ int ifkv_store_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t 
  *
  * The first call allocates the context's memory for partial results of work cut along the cache
  * (later ones allocate nothing); a caller that captures calls into a graph makes one call before.
+ * Calls of one context, and replays of graphs that hold them, share that memory: they must not run at the
+ * same time (two streams, two graphs); a context for each can.
  * Errors: as ifkv_store_pages; IFKV_EINVAL for max_rows < 1; IFKV_ENOMEM.
  */
 int ifkv_attend_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t *page_table, int32_t n_seqs,

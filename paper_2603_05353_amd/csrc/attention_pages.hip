@@ -32,7 +32,7 @@ __device__ __forceinline__ float block_reduce_sum(float v, float *red) {
 // One workgroup for each (row, query head).  256 tokens at a time: every thread forms one logit, the workgroup agrees on the
 // running maximum and sum, then thread t adds to output column t % D over a share of the tokens.
 template <typename Tag, int D>
-__global__ __launch_bounds__(kThreads) void attend_pages_generic_kernel(PageTable t, int max_rows, const uint8_t *__restrict__ k_pages,
+__global__ __launch_bounds__(kThreads) void attend_pages_generic_kernel(PageTable t, int first_row, int n_rows, const uint8_t *__restrict__ k_pages,
                                                                         const uint8_t *__restrict__ v_pages,
                                                                         const float *__restrict__ k_scale, const float *__restrict__ v_scale,
                                                                         int n_pages, int n_q_heads, int n_kv_heads, float sm_scale,
@@ -47,10 +47,11 @@ __global__ __launch_bounds__(kThreads) void attend_pages_generic_kernel(PageTabl
   __shared__ float s_o[kThreads];
   const int tid = threadIdx.x, h = blockIdx.y, g = h / (n_q_heads / n_kv_heads);
   int lo, hi;
-  const int s = static_cast<int>(blockIdx.x / max_rows);
+  const int s = static_cast<int>(blockIdx.x / n_rows);
   rows_of(t, s, lo, hi);
-  const int r = lo + static_cast<int>(blockIdx.x % max_rows);
-  if (r >= hi) return;
+  const int i = first_row + static_cast<int>(blockIdx.x % n_rows);
+  if (i >= hi - lo) return;
+  const int r = lo + i;
   const int64_t row_head = static_cast<int64_t>(r) * n_q_heads + h;
   const int p = t.row_pos[r];
   const bool seen = p >= 0 && (p >> 6) < t.width;
@@ -104,18 +105,21 @@ template <typename Tag, int D>
 hipError_t run_generic(ifkv_ctx *ctx, const ifkv_page_cache &pages, PageTable t, int max_rows, const void *q, int64_t q_stride, void *out,
                        float *lse_out) {
   const auto &d = ctx->desc;
-  // a grid has fewer than 2^32 threads: so many sequences a launch
-  const int step = std::max(1, (1 << 23) / max_rows);
+  // a grid has fewer than 2^32 threads: so many rows of a sequence, and so many sequences, a launch
+  constexpr int kMost = 1 << 23;
+  const int rows = std::min(max_rows, kMost), step = kMost / rows;
   const int64_t e = static_cast<int64_t>(dtype_size(d.dtype));
-  for (int s = 0; s < t.n_seqs; s += step) {
-    const PageTable u = t.from(s, std::min(step, t.n_seqs - s));
-    const int64_t skip = t.row_start != nullptr ? 0 : s;  // rows of the sequences before, where each has one
-    hipLaunchKernelGGL((attend_pages_generic_kernel<Tag, D>), dim3(static_cast<unsigned>(u.n_seqs) * max_rows, d.n_q_heads), dim3(kThreads),
-                       0, ctx->stream, u, max_rows, static_cast<const uint8_t *>(pages.k), static_cast<const uint8_t *>(pages.v),
-                       pages.k_scale, pages.v_scale, static_cast<int>(pages.n_pages), d.n_q_heads, d.n_kv_heads, ctx->sm_scale,
-                       static_cast<const char *>(q) + skip * q_stride * e, q_stride, static_cast<char *>(out) + skip * d.n_q_heads * D * e,
-                       lse_out != nullptr ? lse_out + skip * d.n_q_heads : nullptr);
-  }
+  for (int s = 0; s < t.n_seqs; s += step)
+    for (int r = 0; r < max_rows; r += rows) {
+      const PageTable u = t.from(s, std::min(step, t.n_seqs - s));
+      const int n = std::min(rows, max_rows - r);
+      const int64_t skip = t.row_start != nullptr ? 0 : s;  // rows of the sequences before, where each has one
+      hipLaunchKernelGGL((attend_pages_generic_kernel<Tag, D>), dim3(static_cast<unsigned>(u.n_seqs) * n, d.n_q_heads), dim3(kThreads), 0,
+                         ctx->stream, u, r, n, static_cast<const uint8_t *>(pages.k),
+                         static_cast<const uint8_t *>(pages.v), pages.k_scale, pages.v_scale, static_cast<int>(pages.n_pages), d.n_q_heads,
+                         d.n_kv_heads, ctx->sm_scale, static_cast<const char *>(q) + skip * q_stride * e, q_stride,
+                         static_cast<char *>(out) + skip * d.n_q_heads * D * e, lse_out != nullptr ? lse_out + skip * d.n_q_heads : nullptr);
+    }
   return hipGetLastError();
 }
 

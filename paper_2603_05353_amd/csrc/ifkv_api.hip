@@ -588,6 +588,7 @@ int ifkv_rope_rows_axes(ifkv_ctx *ctx, void *x, const int32_t *pos, int32_t n_ax
   if (ctx == nullptr) return IFKV_EINVAL;
   if (n_rows < 0 || n_heads <= 0) return fail(ctx, IFKV_EINVAL, "rope_rows_axes: n_rows must be >= 0 and n_heads > 0");
   if (n_rows >= (int64_t(1) << 31)) return fail(ctx, IFKV_ESHAPE, "rope_rows_axes: too many rows");
+  if (n_heads > INT32_MAX / ctx->desc.head_dim) return fail(ctx, IFKV_ESHAPE, "rope_rows_axes: too many heads");
   if (n_axes < 1 || n_axes > IFKV_MAX_AXES)
     return fail(ctx, IFKV_EINVAL, "rope_rows_axes: n_axes=%d is outside [1, %d]", n_axes, IFKV_MAX_AXES);
   if (axis_of_pair == nullptr) return fail(ctx, IFKV_EINVAL, "rope_rows_axes: axis_of_pair is NULL");

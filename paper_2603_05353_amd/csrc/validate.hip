@@ -23,12 +23,19 @@ __global__ void check_ascending_kernel(const int32_t *__restrict__ v, int64_t n,
     if (v[i] <= v[i - 1]) atomicMin(first_bad, static_cast<int>(i));
 }
 
-// first_bad: smallest i that is not above the entry before it in the same sequence; negative entries name no token
+// first_bad: smallest i that is not above the entry before it in the same sequence.  Negative entries name no token and stand at a
+// sequence's beginning or end: the first after such an end that names one is bad too.
 __global__ void check_page_rows_kernel(PageTable t, int *first_bad) {
   for (int64_t s = blockIdx.x; s < t.n_seqs; s += gridDim.x) {
     const int64_t lo = max(t.row_start[s], 0), hi = min(static_cast<int64_t>(t.row_start[s + 1]), t.n_rows);
     for (int64_t i = lo + 1 + threadIdx.x; i < hi; i += blockDim.x)
-      if (t.row_pos[i] >= 0 && t.row_pos[i] <= t.row_pos[i - 1]) atomicMin(first_bad, static_cast<int>(i));
+      if (t.row_pos[i] >= 0 && t.row_pos[i] <= t.row_pos[i - 1]) {
+        atomicMin(first_bad, static_cast<int>(i));
+      } else if (t.row_pos[i] < 0 && t.row_pos[i - 1] >= 0) {
+        int64_t j = i + 1;
+        while (j < hi && t.row_pos[j] < 0) ++j;
+        if (j < hi) atomicMin(first_bad, static_cast<int>(j));
+      }
   }
 }
 

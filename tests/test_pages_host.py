@@ -193,6 +193,12 @@ def test_rope_rows_axes_refusals(layer):
     assert call(layer._ctx, None, None, 3, ap, 0, 40, 0) == 0
 
 
+def test_rope_rows_axes_refuses_rows_that_pass_32_bits(layer):
+    axes = (C.c_int32 * 64)()
+    rc = layer._lib.ifkv_rope_rows_axes(layer._ctx, fake(), fake(), 1, C.cast(axes, C.c_void_p), 4, 1 << 24, 0)
+    refused(layer, rc, B.IFKV_ESHAPE, "too many heads")      # 2^24 heads of 128
+
+
 def test_binding_takes_no_tensor_of_another_kind(layer):
     """What the C call cannot see: devices, types, shapes and layouts (CPU tensors stand for the wrong device)."""
     f8 = torch.float8_e4m3fn
