@@ -98,4 +98,5 @@ def assert_attended(out, lse, ref, dtype, n, parts):
         empty = np.isneginf(want_lse)
         assert np.array_equal(np.isneginf(lse)[rows], empty[rows])
         ok = rows[:, None] & ~empty
-        assert (np.abs(lse - want_lse)[ok] <= bound_lse[ok]).all(), np.abs(lse - want_lse)[ok].max()
+        off = np.abs(lse[ok] - want_lse[ok])
+        assert (off <= bound_lse[ok]).all(), off.max()
