@@ -452,8 +452,8 @@ int ifkv_store_pages(ifkv_ctx *ctx, const ifkv_page_cache *pages, const int32_t 
  *
  * Logits, exponentials and sums are fp32; keys and values are exact in the products.  bf16 layers:
  * queries enter the first product as they are, probabilities the second as the sum of two bf16
- * numbers (16 bits; one, 8 bits, where sequences bring more than 64 query columns per kv head).  fp32
- * layers: both as the sum of three.
+ * numbers (16 bits; one, 8 bits, where sequences bring more than 32 query columns, max_rows * G, per kv
+ * head).  fp32 layers: both as the sum of three.
  *
  *   row_start  as above; rows behind row_start[n_seqs] are neither read nor written in out and lse_out
  *   max_rows   no sequence has more rows than this (1 without row_start); rows beyond are not computed.  The work that a

@@ -12,7 +12,7 @@
 //
 // Measured on one MI355X, a call with its join, where reading alone reaches 6.2 to 6.9 TB/s and a large bf16 product 1.2 PFLOP/s: 64 sequences
 // of 0.8K to 8K tokens, 32/8 heads of 128, 597 MB in 109 us (the kernel alone 6.0 TB/s); one of 130K tokens 52 us (266 MB); 35 columns of
-// 12 sequences of up to 20K 62 us (195 MB); 512 rows over 32K 265 us (1.03 PFLOP/s); 300 tokens of one sequence 7.5 us, all of it
+// 12 sequences of up to 20K 57 us (195 MB); 512 rows over 32K 265 us (1.03 PFLOP/s); 300 tokens of one sequence 7.5 us, all of it
 // latency: positions, table, scales and pages are each asked for with the answer to the one before.
 #include <algorithm>
 
@@ -37,6 +37,14 @@ template <typename Tag>
 constexpr int kQueryParts = 3;
 template <>
 constexpr int kQueryParts<BF16Tag> = 1;
+
+// bf16 numbers that hold a probability in the second product, by tiles of 16 columns.  bf16 layers: two where memory bounds the call, up to
+// 32 columns (8 rows of 12 sequences of up to 20K tokens 80 us, with one 78); one, like the result, where instructions do (35 columns
+// 57 us, with two 63; 64 columns 105, with two 116).
+template <typename Tag>
+constexpr int weight_parts(int tiles) {
+  return kQueryParts<Tag> > 1 ? 3 : tiles <= 2 ? 2 : 1;
+}
 
 // Partial results of a piece of an item: accumulators as the wavefronts hold them, then reference and sum of every column.
 template <int D, int NT>
@@ -438,8 +446,7 @@ constexpr int kFewWaves = NT * kQueryParts<Tag> * D <= 256 || NT == 1 ? 2 : 1;
 
 template <typename Tag, int D, int NT>
 __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void attend_pages_kernel(AttendArgs a, Image<D, NT> *__restrict__ partials) {
-  constexpr int PP = kQueryParts<Tag> == 1 ? 2 : 3;
-  using Cols = Columns<Tag, D, NT, PP, (NT > 1)>;
+  using Cols = Columns<Tag, D, NT, weight_parts<Tag>(NT), (NT > 1)>;
   constexpr int KV = Cols::KV, DT = Cols::DT, TILE = kPageTokens * D;
   constexpr int LOADS = TILE / 1024;   // of 1 KiB, for a page's keys or values
   __shared__ AttendPlanMemory plan_memory;
@@ -581,9 +588,9 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
 // ---------------------------------------------------------------------------
 constexpr int kPageList = kAttendThreads;   // pages whose places are looked up together
 
-template <typename Tag, int D, int NT, int PP>
+template <typename Tag, int D, int NT>
 __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(AttendArgs a, Image<D, 4 * NT> *__restrict__ partials) {
-  using Cols = Columns<Tag, D, NT, PP, true>;
+  using Cols = Columns<Tag, D, NT, weight_parts<Tag>(4 * NT), true>;
   constexpr int KV = Cols::KV, DT = Cols::DT, KS = Cols::KS, TILE = kPageTokens * D;
   constexpr int LOADS = 2 * TILE / 1024;              // of 1 KiB, a page: keys first
   constexpr int MINE = LOADS / kAttendWaves;          // of a wavefront
@@ -852,7 +859,7 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
     const dim3 block(kAttendThreads);
     const dim3 grid = cut ? dim3(workgroups) : dim3(static_cast<unsigned>(static_cast<int64_t>(a.t.n_seqs) * plan.n_blocks), d.n_kv_heads);
     if constexpr (TILES >= 4) {
-      hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4, TILES == 4 ? 2 : 1>), grid, block, 0, ctx->stream, a, partials);
+      hipLaunchKernelGGL((attend_pages_block_kernel<Tag, D, TILES / 4>), grid, block, 0, ctx->stream, a, partials);
     } else {
       hipLaunchKernelGGL((attend_pages_kernel<Tag, D, TILES>), grid, block, 0, ctx->stream, a, partials);
     }
@@ -870,12 +877,11 @@ hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTa
                        void *out, float *lse_out) {
   const int64_t columns = static_cast<int64_t>(max_rows) * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads);
   // A wavefront with all columns converts a page's elements itself, alone and at its own pace; from four tiles on its registers do not
-  // suffice, and blocks share the pages (12 sequences of up to 20K: 35 columns 62 us, as a block 65; 64 columns as a block 116).
+  // suffice, and blocks share the pages (12 sequences of up to 20K: 35 columns 57 us, as a block 61; 64 columns as a block 105).
   if (columns <= 16) return run<Tag, D, 1>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if (columns <= 32 || kQueryParts<Tag> > 1) return run<Tag, D, 2>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if constexpr (kQueryParts<Tag> == 1) {
     if (columns <= 48) return run<Tag, D, 3>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
-    // probabilities as two bf16 numbers; from here on the matrix cores bound the call, not memory, and one has to do
     if (columns <= 64) return run<Tag, D, 4>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
     return run<Tag, D, 8>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   }

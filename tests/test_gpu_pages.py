@@ -23,7 +23,7 @@ def layer(dtype, hq, hkv, d, max_ctx=1 << 20, **kw):
 
 def parts_of(dtype, columns):
     """bf16 numbers that hold a weight in the second product."""
-    return 3 if dtype == "f32" else 2 if columns <= 64 else 1
+    return 3 if dtype == "f32" else 2 if columns <= 32 else 1
 
 
 # ---- rotary positions ---------------------------------------------------------------------------------------------
@@ -353,8 +353,8 @@ def test_attend_pages_max_rows_bounds_what_is_computed():
     out = torch.full_like(full, 3.0)
     L.attend_pages(q, i32(pos), pool_to_device(pool), i32(table), row_start=i32(start), max_rows=6, out=out)
     ref = P.attend_pages(q64, pos, pool, table, 128 ** -0.5, row_start=start)
-    for o in (full, out):
-        assert_attended(to_host_f64(o, "bf16"), None, ref, "bf16", 192, 2)
+    for o, rows in ((full, 9), (out, 6)):            # 36 columns: a weight is one bf16 number, 2^-8 of the mass; 24: two, 2^-16
+        assert_attended(to_host_f64(o, "bf16"), None, ref, "bf16", 192, parts_of("bf16", rows * 4))
     L.close()
 
 
