@@ -452,7 +452,7 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
   __shared__ AttendPlanMemory plan_memory;
   __shared__ union {
     v4u tile[kAttendWaves][2][LOADS][64];   // keys and values of a page
-    Image<D, NT> image[2];
+    Image<D, NT> image[kAttendWaves];
   } mem;
   const PageTable &t = a.t;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -541,35 +541,44 @@ __global__ __launch_bounds__(kAttendThreads, (kFewWaves<Tag, D, NT>)) void atten
       }
     }
     c.complete();
-    // wavefronts 2 and 3 into 0 and 1, then 1 into 0
+    // each wavefront joins a quarter of the output rows of all four
+    __syncthreads();   // (the tiles have been read)
+    c.save(mem.image[wave], 0);
+    __syncthreads();
 #pragma unroll
-    for (int half = 2; half >= 1; half >>= 1) {
-      __syncthreads();   // (the tiles, or the images of the step before)
-      if (wave >= half && wave < 2 * half) c.save(mem.image[wave - half], 0);
-      __syncthreads();
-      if (wave < half) {
-        const Image<D, NT> &im = mem.image[wave];
+    for (int nt = 0; nt < NT; ++nt) {
+      constexpr int MINE = DT / kAttendWaves;
+      float by[kAttendWaves], ref = -INFINITY, sum = 0.f;
+      f32x4 o[MINE];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float other = im.ref[nt][c.n], m = fmaxf(c.ref[nt], other);
-          const float x = c.ref[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.ref[nt] - m);
-          const float y = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - m);
-          c.ref[nt] = m;
-          c.sum[nt] = c.sum[nt] * x + im.sum[nt][c.n] * y;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const f32x4 o = im.o[dt * NT + nt][lane];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) c.o[dt][nt][e] = c.o[dt][nt][e] * x + o[e] * y;
-          }
-        }
+      for (int w = 0; w < kAttendWaves; ++w) {
+        by[w] = mem.image[w].ref[nt][c.n];
+        ref = fmaxf(ref, by[w]);
       }
-    }
-    if (wave == 0) {
-      if (slot < 0)
-        c.finish(a.out, a.lse_out);
-      else
-        c.save(partials[slot], 0);
+#pragma unroll
+      for (int w = 0; w < kAttendWaves; ++w) {
+        by[w] = by[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(by[w] - ref);
+        sum = fmaf(mem.image[w].sum[nt][c.n], by[w], sum);
+      }
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        const int at = (wave * MINE + i) * NT + nt;
+        o[i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kAttendWaves; ++w) {
+          const f32x4 x = mem.image[w].o[at][lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][e] = fmaf(x[e], by[w], o[i][e]);
+        }
+        if (slot >= 0) partials[slot].o[at][lane] = o[i];
+      }
+      if (slot < 0) {
+        if (c.row_head[nt] >= 0)
+          write_columns<Tag, D, MINE>(a.out, wave == 0 ? a.lse_out : nullptr, c.row_head[nt], wave * MINE, c.g, o, 1, ref, sum);
+      } else if (wave == 0 && c.g == 0) {
+        partials[slot].ref[nt][c.n] = ref;
+        partials[slot].sum[nt][c.n] = sum;
+      }
     }
     __syncthreads();   // the images are given up
   };
