@@ -726,17 +726,19 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_pages_block_kernel(A
 }
 
 // Joins the pieces of an item: a workgroup for a quarter of the output rows of a tile of 16 columns.  Its wavefronts take the
-// pieces in turn, eight requests under way, and join.
+// pieces in turn, eight requests under way, and join.  One wavefront where eight requests are about all pieces there are (64 sequences of up to
+// 8K tokens, 512 items in 256 shares: 106.4 us a call, with four 108.1; 512 rows, 128 in 512: 264 and 268), four where there are more (one of
+// 130K, 8 in 256: 51.5, with one 53.7).
 constexpr int kMergeSplit = 4, kMergeBatch = 8;
 
-template <typename Tag, int D, int NT>
-__global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(PageTable t, AttendPlan plan, int max_rows, int n_q_heads,
+template <typename Tag, int D, int NT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void attend_pages_merge_kernel(PageTable t, AttendPlan plan, int max_rows, int n_q_heads,
                                                                             const int *__restrict__ item_start,
                                                                             const Image<D, NT> *__restrict__ partials,
                                                                             void *__restrict__ out, float *__restrict__ lse_out) {
   constexpr int DT = D / 16 / kMergeSplit;
-  __shared__ f32x4 s_o[kAttendWaves - 1][DT][64];
-  __shared__ float s_ref[kAttendWaves][16], s_sum[kAttendWaves][16];
+  __shared__ f32x4 s_o[WAVES][DT][64];   // (the first one's is not used)
+  __shared__ float s_ref[WAVES][16], s_sum[WAVES][16];
   const int item = blockIdx.x / (NT * kMergeSplit), nt = blockIdx.x / kMergeSplit % NT, quarter = blockIdx.x % kMergeSplit;
   const int h = blockIdx.y;
   const uint32_t s = item_start[item], e = item_start[item + 1], total = item_start[t.n_seqs * plan.n_blocks];
@@ -751,12 +753,12 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
   f32x4 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0, 0, 0, 0};
-  for (int p0 = wave; p0 < pieces; p0 += kAttendWaves * kMergeBatch) {
+  for (int p0 = wave; p0 < pieces; p0 += WAVES * kMergeBatch) {
     float refs[kMergeBatch], sums[kMergeBatch];
     f32x4 x[kMergeBatch][DT];
 #pragma unroll
     for (int u = 0; u < kMergeBatch; ++u) {
-      const int p = p0 + u * kAttendWaves;
+      const int p = p0 + u * WAVES;
       refs[u] = -INFINITY;
       sums[u] = 0.f;
 #pragma unroll
@@ -789,30 +791,32 @@ __global__ __launch_bounds__(kAttendThreads) void attend_pages_merge_kernel(Page
         for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(x[u][dt][e], b, o[dt][e]);
     }
   }
-  if (g == 0) s_ref[wave][n] = ref, s_sum[wave][n] = sum;
-  if (wave > 0)
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) s_o[wave - 1][dt][lane] = o[dt];
-  __syncthreads();
-  if (wave > 0) return;
   float top = ref;
+  if constexpr (WAVES > 1) {
+    if (g == 0) s_ref[wave][n] = ref, s_sum[wave][n] = sum;
+    if (wave > 0)
 #pragma unroll
-  for (int w = 1; w < kAttendWaves; ++w) top = fmaxf(top, s_ref[w][n]);
-  const float a = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top);
-  sum *= a;
+      for (int dt = 0; dt < DT; ++dt) s_o[wave][dt][lane] = o[dt];
+    __syncthreads();
+    if (wave > 0) return;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, s_ref[w][n]);
+    const float a = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top);
+    sum *= a;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[dt][e] *= a;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-  for (int w = 1; w < kAttendWaves; ++w) {
-    const float b = s_ref[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_ref[w][n] - top);
-    sum = fmaf(s_sum[w][n], b, sum);
+      for (int e = 0; e < 4; ++e) o[dt][e] *= a;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const f32x4 x = s_o[w - 1][dt][lane];
+    for (int w = 1; w < WAVES; ++w) {
+      const float b = s_ref[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_ref[w][n] - top);
+      sum = fmaf(s_sum[w][n], b, sum);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(x[e], b, o[dt][e]);
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 x = s_o[w][dt][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[dt][e] = fmaf(x[e], b, o[dt][e]);
+      }
     }
   }
   const AttendItem rows(t, plan, max_rows, item);
@@ -876,8 +880,14 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
     if (e != hipSuccess) return e;
   }
   if (!cut) return hipSuccess;
-  hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, TILES>), dim3(static_cast<unsigned>(items * TILES * kMergeSplit), d.n_kv_heads),
-                     dim3(kAttendThreads), 0, ctx->stream, t, plan, max_rows, d.n_q_heads, item_start, partials, out, lse_out);
+  const dim3 grid(static_cast<unsigned>(items * TILES * kMergeSplit), d.n_kv_heads);
+  if (workgroups <= kMergeBatch * items * d.n_kv_heads) {
+    hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, TILES, 1>), grid, dim3(64), 0, ctx->stream, t, plan, max_rows, d.n_q_heads, item_start,
+                       partials, out, lse_out);
+  } else {
+    hipLaunchKernelGGL((attend_pages_merge_kernel<Tag, D, TILES, kAttendWaves>), grid, dim3(kAttendThreads), 0, ctx->stream, t, plan, max_rows,
+                       d.n_q_heads, item_start, partials, out, lse_out);
+  }
   return hipGetLastError();
 }
 
