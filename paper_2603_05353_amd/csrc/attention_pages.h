@@ -25,6 +25,7 @@ struct AttendPlan {
   int group;          // query heads of a kv head
   int units;          // at most; 0: not cut, a workgroup takes the item blockIdx.x of kv head blockIdx.y
   int least_pages;    // of a unit
+  int start_pages;    // what beginning an item costs, in pages: so many stand before its own in the list, and nobody reads them
 };
 
 // Shares: unit u has the pages [edge(u), edge(u + 1)) of the list of n.
@@ -74,7 +75,7 @@ __device__ __forceinline__ int item_lanes(const AttendPlan &plan, int max_rows) 
 }
 
 struct AttendPlanMemory {
-  int start[kMaxItems + 1];   // pages of a kv head before an item
+  int start[kMaxItems + 1];   // pages of a kv head in the list before an item
   int scan[kAttendWaves];
 };
 
@@ -88,7 +89,7 @@ __device__ __forceinline__ void add_up_items(const PageTable &t, const AttendPla
     const int i = i0 + tid / lanes;
     if (i >= n_items) continue;   // (the lanes of an item go together)
     const int n = item_pages(t, plan, max_rows, i, tid & (lanes - 1), lanes);
-    if ((tid & (lanes - 1)) == 0) mem.start[i] = n;
+    if ((tid & (lanes - 1)) == 0) mem.start[i] = n > 0 ? n + plan.start_pages : 0;
   }
   __syncthreads();
   constexpr int PER = kMaxItems / kAttendThreads;   // neighbouring items of a thread

@@ -424,9 +424,10 @@ __device__ __forceinline__ void each_piece(const AttendPlan &plan, int n_items, 
   while (x < end) {
     const uint32_t s = scalar(mem.start[item]), e = scalar(mem.start[item + 1]);
     if (s < e) {
-      const uint32_t last = min(e, r + (end - x));
-      piece(item, static_cast<int>(h), static_cast<int>(r - s), static_cast<int>(last - s),
-            r == s && last == e ? -1 : static_cast<int>(2 * unit + (r == s ? 1 : 0)));
+      const uint32_t last = min(e, r + (end - x)), own = s + plan.start_pages, p = max(r, own);
+      if (p < last)
+        piece(item, static_cast<int>(h), static_cast<int>(p - own), static_cast<int>(last - own),
+              p == own && last == e ? -1 : static_cast<int>(2 * unit + (p == own ? 1 : 0)));
       x += last - r;
       r = last;
     }
@@ -733,9 +734,9 @@ constexpr int kMergeSplit = 4, kMergeBatch = 8;
 
 template <typename Tag, int D, int NT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attend_pages_merge_kernel(PageTable t, AttendPlan plan, int max_rows, int n_q_heads,
-                                                                            const int *__restrict__ item_start,
-                                                                            const Image<D, NT> *__restrict__ partials,
-                                                                            void *__restrict__ out, float *__restrict__ lse_out) {
+                                                                        const int *__restrict__ item_start,
+                                                                        const Image<D, NT> *__restrict__ partials, void *__restrict__ out,
+                                                                        float *__restrict__ lse_out) {
   constexpr int DT = D / 16 / kMergeSplit;
   __shared__ f32x4 s_o[WAVES][DT][64];   // (the first one's is not used)
   __shared__ float s_ref[WAVES][16], s_sum[WAVES][16];
@@ -744,7 +745,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_pages_merge_kernel(PageTabl
   const uint32_t s = item_start[item], e = item_start[item + 1], total = item_start[t.n_seqs * plan.n_blocks];
   if (s == e) return;
   const Shares shares(plan, total * gridDim.y);
-  const uint32_t u0 = shares.unit_of(h * total + s), u1 = shares.unit_of(h * total + e - 1);
+  const uint32_t u0 = shares.unit_of(h * total + s + plan.start_pages), u1 = shares.unit_of(h * total + e - 1);
   const int pieces = static_cast<int>(u1 - u0) + 1;
   if (pieces == 1) return;   // the unit wrote the result
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
@@ -842,6 +843,7 @@ constexpr int kWholePages = 64, kWholePagesFewItems = 20, kManyItems = 256;
 // pages (512 rows over 32K: 303 us, with one 497).
 constexpr int kTeams = 256, kBlockTeams = 512;
 constexpr int kLeastPages = kAttendWaves;   // of a unit: one for each wavefront
+constexpr int kStartPages = 4, kBlockStartPages = 2;
 
 template <typename Tag, int D, int TILES>
 hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int max_rows, const void *q, int64_t q_stride, void *out,
@@ -852,9 +854,11 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
   plan.columns = TILES * 16;
   plan.n_blocks = static_cast<int>((static_cast<int64_t>(max_rows) * plan.group + plan.columns - 1) / plan.columns);
   plan.least_pages = kLeastPages;
+  plan.start_pages = TILES < 4 ? kStartPages : kBlockStartPages;
   const int64_t items = static_cast<int64_t>(t.n_seqs) * plan.n_blocks;
   // (pages are added up in 32 bits)
-  const bool cut = t.width > (items * d.n_kv_heads >= kManyItems ? kWholePages : kWholePagesFewItems) && items <= kMaxItems && items * t.width < INT32_MAX / d.n_kv_heads;
+  const bool cut = t.width > (items * d.n_kv_heads >= kManyItems ? kWholePages : kWholePagesFewItems) && items <= kMaxItems &&
+                   items * (t.width + int64_t(plan.start_pages)) < INT32_MAX / d.n_kv_heads;
   const int workgroups = TILES < 4 ? kTeams : kBlockTeams;
   plan.units = cut ? workgroups : 0;
   int *item_start = static_cast<int *>(ctx->page_partials);
