@@ -843,7 +843,10 @@ constexpr int kWholePages = 64, kWholePagesFewItems = 20, kManyItems = 256;
 // pages (512 rows over 32K: 303 us, with one 497).
 constexpr int kTeams = 256, kBlockTeams = 512;
 constexpr int kLeastPages = kAttendWaves;   // of a unit: one for each wavefront
-constexpr int kStartPages = 4, kBlockStartPages = 2;
+// What a workgroup that begins an item loses, in pages of those it reads meanwhile elsewhere: positions, queries, first pages, the join.  Without it shares
+// that hold the ends of several items finish last: 64 sequences of up to 8K tokens 106 us, with 8 pages 102 (16: 105); 20 columns of 64 123.6, with 12 116.6
+// (40: 124); 35 columns of 12 sequences 54.4, with 20 49 (40: 51); 36 columns of 64 as blocks 140.8, with 6 130.5 (14: 135).
+constexpr int start_pages(int tiles) { return tiles == 1 ? 8 : tiles == 2 ? 12 : tiles == 3 ? 20 : 6; }
 
 template <typename Tag, int D, int TILES>
 hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int max_rows, const void *q, int64_t q_stride, void *out,
@@ -854,7 +857,7 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
   plan.columns = TILES * 16;
   plan.n_blocks = static_cast<int>((static_cast<int64_t>(max_rows) * plan.group + plan.columns - 1) / plan.columns);
   plan.least_pages = kLeastPages;
-  plan.start_pages = TILES < 4 ? kStartPages : kBlockStartPages;
+  plan.start_pages = start_pages(TILES);
   const int64_t items = static_cast<int64_t>(t.n_seqs) * plan.n_blocks;
   // (pages are added up in 32 bits)
   const bool cut = t.width > (items * d.n_kv_heads >= kManyItems ? kWholePages : kWholePagesFewItems) && items <= kMaxItems &&
