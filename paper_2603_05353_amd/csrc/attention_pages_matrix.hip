@@ -831,11 +831,12 @@ __global__ __launch_bounds__(WAVES * 64) void attend_pages_merge_kernel(PageTabl
 constexpr size_t kTableBytes = (kMaxItems + 4) / 4 * 4 * sizeof(int);
 
 // The longest sequences, in pages, whose items are taken whole by a workgroup each.  Without cuts there is nothing to plan and to
-// join, 6 to 10 us less; what is lost is time at the end, when only the longest are left, and chips that are not full.  With a
-// workgroup for every CU or more, up to 64 pages (200 sequences of up to 1.5K tokens 72 us instead of 97, 32 of up to 2K 23
-// instead of 32; 64 of up to 8K, 128 pages, 141 instead of 109); otherwise up to 20 (one of 1000 tokens 10.6 us instead of 13.7, of
-// 2000 20 instead of 14).
-constexpr int kWholePages = 64, kWholePagesFewItems = 20, kManyItems = 256;
+// join, 6 to 10 us less; what is lost is time at the end, when only the longest are left, and chips that are not full.  Whole / cut, us:
+//   a workgroup for every CU or more, up to 48 columns: 24 pages (200 sequences) 68 / 79, 32 pages (32 sequences) 22.1 / 26.9, 47 pages
+//     (32, 64 and 128 sequences) 28.6 / 29.9, 54.6 / 49.4, 99 / 88, 63 pages (64) 71 / 60;  blocks: 32 pages 53 / 64, 47 pages 35 / 45 and 69 / 72.6;
+//   fewer: 16 pages (one sequence) 10.3 / 12.4, 32 pages 20 / 14;  blocks: 5 pages 12.3 / 15.8, 8 pages 15.3 / 15.9, 12 pages 19.0 / 16.0.
+constexpr int kManyItems = 256;
+constexpr int whole_pages(int tiles, bool many) { return many ? (tiles < 4 ? 40 : 64) : (tiles < 4 ? 20 : 8); }
 
 // Workgroups of a launch that is cut: what the chip holds, so that all of them run at once and end together.  One a CU where
 // every wavefront has its own pages (with two a CU half the memory for partial results would be gone again on planning and
@@ -843,9 +844,10 @@ constexpr int kWholePages = 64, kWholePagesFewItems = 20, kManyItems = 256;
 // pages (512 rows over 32K: 303 us, with one 497).
 constexpr int kTeams = 256, kBlockTeams = 512;
 constexpr int kLeastPages = kAttendWaves;   // of a unit: one for each wavefront
-// What a workgroup that begins an item loses, in pages of those it reads meanwhile elsewhere: positions, queries, first pages, the join.  Without it shares
-// that hold the ends of several items finish last: 64 sequences of up to 8K tokens 106 us, with 8 pages 102 (16: 105); 20 columns of 64 123.6, with 12 116.6
-// (40: 124); 35 columns of 12 sequences 54.4, with 20 49 (40: 51); 36 columns of 64 as blocks 140.8, with 6 130.5 (14: 135).
+// What a workgroup that begins an item loses, in pages of those it reads meanwhile elsewhere: positions, queries, first pages, the
+// join.  Without it shares that hold the ends of several items finish last: 64 sequences of up to 8K tokens 106 us, with 8 pages 102
+// (16: 105); 20 columns of 64 123.6, with 12 116.6 (40: 124); 35 columns of 12 sequences 54.4, with 20 49 (40: 51); 36 columns of 64
+// as blocks 140.8, with 6 130.5 (14: 135).
 constexpr int start_pages(int tiles) { return tiles == 1 ? 8 : tiles == 2 ? 12 : tiles == 3 ? 20 : 6; }
 
 template <typename Tag, int D, int TILES>
@@ -860,7 +862,7 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
   plan.start_pages = start_pages(TILES);
   const int64_t items = static_cast<int64_t>(t.n_seqs) * plan.n_blocks;
   // (pages are added up in 32 bits)
-  const bool cut = t.width > (items * d.n_kv_heads >= kManyItems ? kWholePages : kWholePagesFewItems) && items <= kMaxItems &&
+  const bool cut = t.width > whole_pages(TILES, items * d.n_kv_heads >= kManyItems) && items <= kMaxItems &&
                    items * (t.width + int64_t(plan.start_pages)) < INT32_MAX / d.n_kv_heads;
   const int workgroups = TILES < 4 ? kTeams : kBlockTeams;
   plan.units = cut ? workgroups : 0;
