@@ -10,10 +10,10 @@
 // e4m3 numbers become bf16 exactly, two an instruction, with the page's scale multiplied in.  (The e4m3 instruction with scales, queries as
 // two e4m3 numbers, would need no conversion of keys, but its sums are off by up to 2^-15 of sum |q k|, bf16 ones by 2^-22.)
 //
-// Measured on one MI355X, a call with its join, where reading alone reaches 6.2 to 6.9 TB/s and a large bf16 product 1.2 PFLOP/s: 64 sequences
-// of 0.8K to 8K tokens, 32/8 heads of 128, 597 MB in 109 us (the kernel alone 6.0 TB/s); one of 130K tokens 52 us (266 MB); 35 columns of
-// 12 sequences of up to 20K 57 us (195 MB); 512 rows over 32K 265 us (1.03 PFLOP/s); 300 tokens of one sequence 7.5 us, all of it
-// latency: positions, table, scales and pages are each asked for with the answer to the one before.
+// Measured on one MI355X, a call with its join, where reading alone reaches 6.2 to 6.9 TB/s and a large bf16 product 1.2 PFLOP/s: 64
+// sequences of 0.8K to 8K tokens, 32/8 heads of 128, 597 MB in 102 us (the kernel alone 6.2 TB/s); one of 130K tokens 49 to 51 us (266 MB);
+// 35 columns of 12 sequences of up to 20K 47 to 50 us (195 MB); 512 rows over 32K 260 us (1.05 PFLOP/s); 300 tokens of one sequence 7.1 us, all
+// of it latency: positions, table, scales and pages are each asked for with the answer to the one before.
 #include <algorithm>
 
 #include "attention_pages.h"
@@ -38,9 +38,9 @@ constexpr int kQueryParts = 3;
 template <>
 constexpr int kQueryParts<BF16Tag> = 1;
 
-// bf16 numbers that hold a probability in the second product, by tiles of 16 columns.  bf16 layers: two where memory bounds the call, up to
-// 32 columns (8 rows of 12 sequences of up to 20K tokens 80 us, with one 78); one, like the result, where instructions do (35 columns
-// 57 us, with two 63; 64 columns 105, with two 116).
+// bf16 numbers that hold a probability in the second product, by tiles of 16 columns.  bf16 layers: two where memory bounds the call,
+// up to 32 columns (32 columns of 12 sequences of up to 20K tokens 77 us, with one 75); one, like the result, where instructions do
+// (35 columns 50 us, with two 56; 64 columns 98, with two 111).
 template <typename Tag>
 constexpr int weight_parts(int tiles) {
   return kQueryParts<Tag> > 1 ? 3 : tiles <= 2 ? 2 : 1;
@@ -838,10 +838,9 @@ constexpr size_t kTableBytes = (kMaxItems + 4) / 4 * 4 * sizeof(int);
 constexpr int kManyItems = 256;
 constexpr int whole_pages(int tiles, bool many) { return many ? (tiles < 4 ? 40 : 64) : (tiles < 4 ? 20 : 8); }
 
-// Workgroups of a launch that is cut: what the chip holds, so that all of them run at once and end together.  One a CU where
-// every wavefront has its own pages (with two a CU half the memory for partial results would be gone again on planning and
-// joining: one sequence of 130K tokens 55 instead of 52 us, 8 rows of 12 sequences 87 instead of 82), two a CU for blocks that share
-// pages (512 rows over 32K: 303 us, with one 497).
+// Workgroups of a launch that is cut: what the chip holds, so that all of them run at once and end together.  One a CU where every
+// wavefront has its own pages (two a CU begin and join twice as often: one sequence of 130K tokens 54.8 instead of 51.5 us, 64 of up to
+// 8K 111 instead of 102), two a CU for blocks that share pages (512 rows over 32K: 260 us, with one 354).
 constexpr int kTeams = 256, kBlockTeams = 512;
 constexpr int kLeastPages = kAttendWaves;   // of a unit: one for each wavefront
 // What a workgroup that begins an item loses, in pages of those it reads meanwhile elsewhere: positions, queries, first pages, the
@@ -905,7 +904,7 @@ hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTa
                        void *out, float *lse_out) {
   const int64_t columns = static_cast<int64_t>(max_rows) * (ctx->desc.n_q_heads / ctx->desc.n_kv_heads);
   // A wavefront with all columns converts a page's elements itself, alone and at its own pace; from four tiles on its registers do not
-  // suffice, and blocks share the pages (12 sequences of up to 20K: 35 columns 57 us, as a block 61; 64 columns as a block 105).
+  // suffice, and blocks share the pages (12 sequences of up to 20K: 35 columns 50 us, as a block 57; 64 columns as a block 98).
   if (columns <= 16) return run<Tag, D, 1>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if (columns <= 32 || kQueryParts<Tag> > 1) return run<Tag, D, 2>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if constexpr (kQueryParts<Tag> == 1) {
