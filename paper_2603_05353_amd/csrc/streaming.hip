@@ -321,7 +321,8 @@ __global__ __launch_bounds__(kThreads) void rope_rows_kernel(v4u *__restrict__ x
 // ---------------------------------------------------------------------------
 // The same rotation for positions with several axes: the angle of pair j is pos[r][axis[j]] * theta_j.
 // A workgroup owns rows_per_block rows.  Its loads go out first; the (cos, sin) tables of its rows are formed, one angle a
-// thread, while they are on their way.
+// thread, while they are on their way.  Memory bounds it: 20480 rows of 32 heads of 128 in bf16 (336 MB) 72 us, 0.94 of a copy's
+// rate; 64 rows 5 us, a launch and the sine.
 // ---------------------------------------------------------------------------
 constexpr int kAxesAngles = kThreads;  // angles of a workgroup: rows_per_block * d/2 at most
 
@@ -499,7 +500,8 @@ hipError_t launch_rope_rows_axes(ifkv_ctx *ctx, void *x, const int32_t *pos, int
   if (n_rows <= 0 || n_heads <= 0) return hipSuccess;
   const auto &d = ctx->desc;
   const int half = d.head_dim / 2, half_shift = __builtin_ctz(half);
-  // a workgroup of as many rows as it has threads for angles, as soon as those fill the chip
+  // A workgroup of as many rows as it has threads for angles, as soon as those fill the chip (four of 32 heads of 128 / one, us: 1024 rows
+  // 6.9 / 5.5, 4096 rows 13.2 / 15.6, 8192 24.6 / 25.7, 20480 72.4 / 70.2).
   const int most = kAxesAngles / half;
   const int rows_per_block = n_rows >= 1024 * most ? most : 1;
   const int64_t row_bytes = row_stride * static_cast<int64_t>(dtype_size(d.dtype));
