@@ -899,6 +899,8 @@ hipError_t run(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, 
   return hipGetLastError();
 }
 
+constexpr int kShortPages = 4;
+
 template <typename Tag, int D>
 hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTable &t, int max_rows, const void *q, int64_t q_stride,
                        void *out, float *lse_out) {
@@ -908,7 +910,12 @@ hipError_t run_columns(ifkv_ctx *ctx, const ifkv_page_cache &pages, const PageTa
   if (columns <= 16) return run<Tag, D, 1>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if (columns <= 32 || kQueryParts<Tag> > 1) return run<Tag, D, 2>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   if constexpr (kQueryParts<Tag> == 1) {
-    if (columns <= 48) return run<Tag, D, 3>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
+    // 48 columns in a wavefront leave room for one workgroup a CU, blocks for two, and a block's wavefronts begin with a quarter as much each:
+    // blocks where sequences are short, or where they are whole and more than the chip (35 columns of 2 sequences of 128 tokens 8.8 us,
+    // otherwise 10.5; of 80 of 128 tokens 12.7 and 20.6, of 1200 32.5 and 37.0; of 12 of 512 14.7 and 13.5)
+    const bool many = static_cast<int64_t>(t.n_seqs) * ctx->desc.n_kv_heads >= kManyItems;
+    if (columns <= 48 && t.width > (many ? whole_pages(3, true) : kShortPages))
+      return run<Tag, D, 3>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
     if (columns <= 64) return run<Tag, D, 4>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
     return run<Tag, D, 8>(ctx, pages, t, max_rows, q, q_stride, out, lse_out);
   }
